@@ -22,7 +22,7 @@
  *    stream).  Argument errors are detected on the host before anything is
  *    enqueued and returned as a status; nothing is written then.  No C++
  *    exception crosses this interface.  awe_last_error() gives detail.
- *  - Results are bit-exact and do not depend on the launch configuration.
+ *  - Results of the integer products are bit-exact and do not depend on the launch configuration.
  *  - awe_encode, awe_gemm_planes, awe_gemm_exact and awe_gemm_mod enqueue only kernels (no
  *    memset, no copy), so they can be captured into a HIP graph once each has been called
  *    eagerly on the device (the first calls set the GEMM's LDS limit and, for the FP16
@@ -120,7 +120,15 @@ typedef enum awe_encoding {
 } awe_encoding;
 
 typedef enum awe_side { AWE_SIDE_A = 0, AWE_SIDE_B = 1 } awe_side;
-typedef enum awe_dtype { AWE_I32 = 0, AWE_I64 = 1 } awe_dtype;
+typedef enum awe_dtype {
+  AWE_I32 = 0,
+  AWE_I64 = 1,
+  /* element types of the operators of quantised inference, below */
+  AWE_I8 = 2,
+  AWE_F32 = 3,
+  AWE_BF16 = 4,
+  AWE_F16 = 5
+} awe_dtype;
 
 #define AWE_MAX_LIMBS 4
 #define AWE_MAX_PLANES 8
@@ -278,6 +286,103 @@ awe_status awe_gemm_crt(int64_t M, int64_t N, int64_t K, const int64_t* A, int64
                         const int32_t* moduli, int32_t n, int64_t* c128, double* c64, int64_t ldc,
                         void* workspace, size_t ws_bytes, int32_t* d_range_flag,
                         hipStream_t stream);
+
+/* ---- Quantised inference -----------------------------------------------------------------
+   Products with 4-bit weights that carry a scale per group, and attention over keys and values
+   held in 8 bits.  Integers are multiplied as integers or as floating-point numbers that hold them
+   exactly; sums, scales and softmax statistics are FP32, and each result is rounded once to its
+   type (nearest, ties to even).  Results are the same on every run and the same for every row
+   whatever else the call holds, except that they depend on which kernel the sizes select.
+   The calls enqueue only kernels, allocate nothing, keep nothing and need no first call: they
+   can be captured into a graph at any time, and overlap on any streams as long as no call
+   writes what another uses.  Outputs share no memory with inputs or a workspace. */
+
+/* Y = X W^T with 4-bit weights: for i < M, j < N
+     Y[i,j] = x_scales[i] * sum_g w_scales[j,g] * sum_{k in group g} X[i,k] * (u[j,k] - z[j,g]).
+   X is M x K (x_type AWE_BF16, AWE_F16 or AWE_I8, leading dimension ldx).  Row j of W holds the
+   codes u[j,k] in 0..15 of output j: byte W[j*ldw + k/2], the low nibble for even k, ldw >=
+   ceil(K/2) bytes (at an odd K the last high nibble is ignored).  Group g covers indices
+   g*group .. g*group + group - 1; group is a multiple of 32, or at least K (one group); the last
+   group may be short.  w_scales[j*lds + g] has s_type (AWE_F32, AWE_BF16, AWE_F16), zero points
+   zeros[j*ldz + g] are bytes, and NULL stands for 8 everywhere (codes of -8..7).  x_scales: FP32, for
+   AWE_I8 only, NULL for 1.  Y is M x N of y_type (AWE_F32, AWE_BF16, AWE_F16).  Pointers are aligned to
+   their element; rows may begin anywhere.  K = 0 writes zeros.  A NaN or infinity in a row of X
+   reaches that row of Y alone. */
+awe_status awe_gemm_w4(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, awe_dtype x_type,
+                       const float* x_scales, const uint8_t* W, int64_t ldw, const void* w_scales, int64_t lds,
+                       awe_dtype s_type, const uint8_t* zeros, int64_t ldz, int64_t group, void* Y, int64_t ldy,
+                       awe_dtype y_type, hipStream_t stream);
+
+/* A cache of keys and values in 8 bits: `num_blocks` blocks of `block` tokens, `heads` heads of
+   `head_dim`.  k is [num_blocks][heads][block][head_dim] int8, v is [num_blocks][heads][head_dim][block]
+   int8 (a token's values are a column: the second product of attention reads 16 consecutive
+   tokens of one dimension), and k_scales and v_scales are [num_blocks][heads] FP32: a stored q stands
+   for q * scale of its block and head.  block is 16, 32, 64 or 128, head_dim 64, 128 or 256; k and v are
+   aligned to 16 bytes.  The caller owns the memory, fills it by awe_cache_store, and need not clear
+   it first. */
+typedef struct awe_cache {
+  int8_t* k;
+  int8_t* v;
+  float* k_scales;
+  float* v_scales;
+  int64_t num_blocks;
+  int32_t heads, head_dim, block;
+} awe_cache;
+
+/* The sequences of a call.  Row tensors hold `rows` tokens; sequence b's are rows starts[b] ..
+   starts[b+1] - 1, the newest of its lengths[b] tokens (at positions lengths[b] - n .. lengths[b] - 1
+   for n rows); position p lies in block blocks[b*ld_blocks + p / block] of the cache, slot p % block.
+   starts (sequences + 1), lengths and blocks are device int32 arrays, read when the kernels
+   run; max_rows and max_length are host bounds on any n and any length, and ld_blocks * block >=
+   max_length.  The kernels check what they read: a sequence whose rows or length do not fit in
+   [0, rows], max_rows and max_length is left out altogether, a block id outside [0, num_blocks)
+   leaves out the tokens of that block, and either sets *d_range_flag (nullable, never cleared) to a
+   nonzero value.  Rows that belong to no sequence are left as they were.  Sequences may share
+   blocks that the call only reads. */
+typedef struct awe_batch {
+  int32_t sequences;
+  const int32_t* starts;
+  const int32_t* lengths;
+  const int32_t* blocks;
+  int64_t ld_blocks;
+  int64_t rows, max_rows, max_length;
+} awe_batch;
+
+/* Stores the rows of k and v (type AWE_F32, AWE_BF16 or AWE_F16; row i, head h, dimension d at
+   k[i*k_row + h*k_head + d], strides in elements, not negative).  lengths include the rows.  For
+   each block and head that gets rows, with the block's scale s (counted as 0 where the block holds no
+   older token of the sequence):
+     s' = max(s, max|x| / 127),  older tokens: q' = rint(q * (s / s')),  rows: q = rint(x / s')
+   in FP32, within [-127, 127], and q = 0 where s' = 0.  The scale of a block never shrinks while
+   tokens are added to it.  A NaN or infinity is stored as 0 and sets *d_range_flag.  Bytes of a
+   block past the sequence's length keep their contents.  A block that a call writes must
+   belong to one sequence of the call only (else that block's contents are unspecified). */
+awe_status awe_cache_store(const awe_cache* cache, const awe_batch* batch, const void* k, int64_t k_row,
+                           int64_t k_head, const void* v, int64_t v_row, int64_t v_head, awe_dtype type,
+                           int32_t* d_range_flag, hipStream_t stream);
+
+/* The reverse: writes what the tokens of the rows stand for, q * scale, to k and v (types and
+   strides as above; different elements may not share memory).  Rows whose block id is out of
+   range are left as they were. */
+awe_status awe_cache_load(const awe_cache* cache, const awe_batch* batch, void* k, int64_t k_row, int64_t k_head,
+                          void* v, int64_t v_row, int64_t v_head, awe_dtype type, int32_t* d_range_flag,
+                          hipStream_t stream);
+
+/* Attention of the rows over their sequences' cached tokens (store them first).  q and out have
+   q_heads heads, a multiple of the cache's heads (query head h reads cache head h / (q_heads / heads)),
+   type AWE_BF16 or AWE_F16, strides as above:
+     out = softmax_j(scale * q . k_j) v_j  over tokens j < lengths[b], and for causal != 0 up to the row's
+   own position only.  A row without any token gets zeros.  max_length also sets how the tokens are
+   split over workgroups: a bound near the longest length is best.  The weights of the second
+   product are rounded to FP16 (relative to the row's largest).  The workspace
+   (awe_cache_attend_workspace_bytes, aligned to 16 bytes; 0 bytes for most prompts) holds the parts
+   of split sequences until the call's kernels have run. */
+awe_status awe_cache_attend_workspace_bytes(const awe_cache* cache, const awe_batch* batch, int32_t q_heads,
+                                            size_t* bytes);
+awe_status awe_cache_attend(const awe_cache* cache, const awe_batch* batch, const void* q, int64_t q_row,
+                            int64_t q_head, int32_t q_heads, awe_dtype type, float scale, int32_t causal, void* out,
+                            int64_t out_row, int64_t out_head, void* workspace, size_t ws_bytes,
+                            int32_t* d_range_flag, hipStream_t stream);
 
 /* Host.  Static description of a status code. */
 const char* awe_status_string(awe_status s);

@@ -28,6 +28,7 @@ ENCODINGS = {"b13": ENC_B13, "awe6": ENC_AWE6, "awe6_alt": ENC_AWE6ALT, "awe4": 
 # awe_side, awe_dtype
 SIDE_A, SIDE_B = 0, 1
 I32, I64 = 0, 1
+I8, F32, BF16, F16 = 2, 3, 4, 5  # element types of the operators of quantised inference
 
 MAX_LIMBS, MAX_PLANES, MAX_PRODUCTS = 4, 8, 16
 K_PAD = 256  # AWE_K_PAD: stored planes pad the reduction length to a multiple of this
@@ -55,6 +56,20 @@ class EncodingInfo(ctypes.Structure):
         ("k_star", ctypes.c_int64), ("k_seg", ctypes.c_int64),
         ("format_a", ctypes.c_int32 * MAX_PLANES), ("format_b", ctypes.c_int32 * MAX_PLANES),
     ]
+
+
+class CacheStruct(ctypes.Structure):  # awe_cache
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("num_blocks", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("block", ctypes.c_int32)]
+
+
+class BatchStruct(ctypes.Structure):  # awe_batch
+    _fields_ = [("sequences", ctypes.c_int32),
+                ("starts", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("blocks", ctypes.c_void_p),
+                ("ld_blocks", ctypes.c_int64),
+                ("rows", ctypes.c_int64), ("max_rows", ctypes.c_int64), ("max_length", ctypes.c_int64)]
 
 
 class AweError(RuntimeError):
@@ -92,6 +107,13 @@ def lib():
         L.awe_crt_workspace_bytes.argtypes = [_P, _I32, _I64, _I64, _I64, ctypes.POINTER(_SZ)]
         L.awe_gemm_crt.argtypes = [_I64, _I64, _I64, _P, _I64, _P, _I64, _I64, _I64, _P, _I32,
                                    _P, _P, _I64, _P, _SZ, _P, _P]
+        L.awe_gemm_w4.argtypes = [_I64, _I64, _I64, _P, _I64, _I32, _P, _P, _I64, _P, _I64, _I32, _P, _I64,
+                                  _I64, _P, _I64, _I32, _P]
+        L.awe_cache_store.argtypes = [_P, _P, _P, _I64, _I64, _P, _I64, _I64, _I32, _P, _P]
+        L.awe_cache_load.argtypes = [_P, _P, _P, _I64, _I64, _P, _I64, _I64, _I32, _P, _P]
+        L.awe_cache_attend_workspace_bytes.argtypes = [_P, _P, _I32, ctypes.POINTER(_SZ)]
+        L.awe_cache_attend.argtypes = [_P, _P, _P, _I64, _I64, _I32, _I32, ctypes.c_float, _I32, _P, _I64, _I64,
+                                       _P, _SZ, _P, _P]
         L.awe_status_string.argtypes = [_I32]
         L.awe_status_string.restype = ctypes.c_char_p
         L.awe_last_error.argtypes = []
@@ -99,7 +121,9 @@ def lib():
         for name in ("awe_get_encoding_info", "awe_get_plane_table", "awe_plane_bytes", "awe_encode",
                      "awe_gemm_planes", "awe_workspace_bytes", "awe_gemm_exact", "awe_gemm_exact_noalloc",
                      "awe_gemm_mod",
-                     "awe_residues", "awe_crt", "awe_crt_workspace_bytes", "awe_gemm_crt"):
+                     "awe_residues", "awe_crt", "awe_crt_workspace_bytes", "awe_gemm_crt",
+                     "awe_gemm_w4", "awe_cache_store", "awe_cache_load", "awe_cache_attend",
+                     "awe_cache_attend_workspace_bytes"):
             getattr(L, name).restype = _I32
         _lib = L
     return _lib
@@ -262,6 +286,41 @@ def gemm_crt(M, N, K, A, lda, B, ldb, bound_a, bound_b, moduli, c128, c64, ldc, 
                               _ptr(d_range_flag), _stream(stream)), "awe_gemm_crt")
 
 
+# ---- quantised inference (cache and batch: Cache and Batch below, or their structures) ----------
+def _struct(x):
+    return ctypes.addressof(x if isinstance(x, ctypes.Structure) else x.struct) if x is not None else None
+
+
+def gemm_w4(M, N, K, X, ldx, x_type, x_scales, W, ldw, w_scales, lds, s_type, zeros, ldz, group, Y, ldy, y_type,
+            stream=None):
+    _check(lib().awe_gemm_w4(M, N, K, _ptr(X), ldx, x_type, _ptr(x_scales), _ptr(W), ldw, _ptr(w_scales), lds,
+                             s_type, _ptr(zeros), ldz, group, _ptr(Y), ldy, y_type, _stream(stream)), "awe_gemm_w4")
+
+
+def cache_store(cache, batch, k, k_row, k_head, v, v_row, v_head, dtype, d_range_flag=None, stream=None):
+    _check(lib().awe_cache_store(_struct(cache), _struct(batch), _ptr(k), k_row, k_head, _ptr(v), v_row, v_head,
+                                 dtype, _ptr(d_range_flag), _stream(stream)), "awe_cache_store")
+
+
+def cache_load(cache, batch, k, k_row, k_head, v, v_row, v_head, dtype, d_range_flag=None, stream=None):
+    _check(lib().awe_cache_load(_struct(cache), _struct(batch), _ptr(k), k_row, k_head, _ptr(v), v_row, v_head,
+                                dtype, _ptr(d_range_flag), _stream(stream)), "awe_cache_load")
+
+
+def cache_attend_workspace_bytes(cache, batch, q_heads):
+    n = _SZ()
+    _check(lib().awe_cache_attend_workspace_bytes(_struct(cache), _struct(batch), q_heads, ctypes.byref(n)),
+           "awe_cache_attend_workspace_bytes")
+    return n.value
+
+
+def cache_attend(cache, batch, q, q_row, q_head, q_heads, dtype, scale, causal, out, out_row, out_head, workspace,
+                 ws_bytes, d_range_flag=None, stream=None):
+    _check(lib().awe_cache_attend(_struct(cache), _struct(batch), _ptr(q), q_row, q_head, q_heads, dtype, scale,
+                                  causal, _ptr(out), out_row, out_head, _ptr(workspace), ws_bytes,
+                                  _ptr(d_range_flag), _stream(stream)), "awe_cache_attend")
+
+
 # ---- torch conveniences (allocation with torch, then the calls above) -------------
 def matmul_exact(A, B, enc=ENC_AWE6, out_dtype=None, d_range_flag=None):
     """C = A B exactly for int8 CUDA tensors A (M x K) and B (K x N)."""
@@ -305,3 +364,179 @@ def matmul_crt(A, B, moduli, bound_a, bound_b, d_range_flag=None):
     gemm_crt(M, N, K, A, A.stride(0), B, B.stride(0), bound_a, bound_b, moduli, c128, c64, N, ws, ws_n,
              d_range_flag)
     return c128, c64
+
+
+# ---- quantised inference on torch tensors ------------------------------------------------------
+_types = {}  # torch dtype -> awe_dtype, filled when torch is first needed
+
+
+def _dtype(t, allowed):
+    if not _types:
+        import torch
+        _types.update({torch.int8: I8, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    code = _types.get(t)
+    if code not in allowed:
+        raise ValueError("element type %s is not supported here" % t)
+    return code
+
+
+def _on_current_device(*tensors):
+    """The library launches on the current device: its tensors must be there."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != here):
+            raise ValueError("a tensor is not on the current device (cuda:%d)" % here)
+
+
+def _rows_2d(t, what):
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a matrix with adjacent elements in its rows" % what)
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError("rows of %s share memory" % what)
+    return max(t.stride(0), t.shape[1])  # a single row may have any stride
+
+
+def matmul_w4(x, w, scales, group, zeros=None, x_scales=None, out_dtype=None):
+    """Y = X W^T for CUDA tensors: x (M x K, bfloat16, float16 or int8), w (N x ceil(K / 2), uint8, two
+    codes per byte, the low nibble first), scales and zeros (N x ceil(K / group); zeros uint8 or None
+    for 8), x_scales (M float32, int8 x only).  out_dtype: x's type, bfloat16 for int8, if not given."""
+    import torch
+    if x.dim() != 2 or w.dim() != 2 or scales.dim() != 2:
+        raise ValueError("x, w and scales must be matrices")
+    M, K = x.shape
+    N = w.shape[0]
+    if group <= 0:
+        raise ValueError("group must be positive")
+    groups = -(-K // group)
+    x_type = _dtype(x.dtype, (BF16, F16, I8))
+    s_type = _dtype(scales.dtype, (F32, BF16, F16))
+    out_dtype = out_dtype or (torch.bfloat16 if x_type == I8 else x.dtype)
+    y_type = _dtype(out_dtype, (F32, BF16, F16))
+    if w.dtype != torch.uint8 or w.shape[1] != (K + 1) // 2:
+        raise ValueError("w must be uint8 of N x ceil(K / 2)")
+    if tuple(scales.shape) != (N, groups) or (zeros is not None and tuple(zeros.shape) != (N, groups)):
+        raise ValueError("scales and zeros must be N x ceil(K / group)")
+    if zeros is not None and zeros.dtype != torch.uint8:
+        raise ValueError("zeros must be uint8")
+    if x_scales is not None and (x_scales.dtype != torch.float32 or tuple(x_scales.shape) != (M,)
+                                 or not x_scales.is_contiguous()):
+        raise ValueError("x_scales must be M float32 values")
+    _on_current_device(x, w, scales, zeros, x_scales)
+    y = torch.empty((M, N), dtype=out_dtype, device=x.device)
+    gemm_w4(M, N, K, x, _rows_2d(x, "x"), x_type, x_scales, w, _rows_2d(w, "w"), scales, _rows_2d(scales, "scales"),
+            s_type, zeros, 0 if zeros is None else _rows_2d(zeros, "zeros"), group, y, N, y_type)
+    return y
+
+
+class Cache:
+    """An int8 cache of keys and values on CUDA tensors: k (blocks x heads x block x dim) and v (blocks x
+    heads x dim x block) int8, k_scales and v_scales (blocks x heads) float32, all contiguous.  Keeps
+    the tensors alive; ``Cache.empty`` allocates them."""
+
+    def __init__(self, k, v, k_scales, v_scales):
+        import torch
+        if k.dim() != 4 or v.dim() != 4:
+            raise ValueError("k and v have four dimensions")
+        blocks, heads, block, dim = k.shape
+        if tuple(v.shape) != (blocks, heads, dim, block) or k.dtype != torch.int8 or v.dtype != torch.int8:
+            raise ValueError("k must be int8 of blocks x heads x block x dim, v of blocks x heads x dim x block")
+        for s in (k_scales, v_scales):
+            if tuple(s.shape) != (blocks, heads) or s.dtype != torch.float32:
+                raise ValueError("scales must be float32 of blocks x heads")
+        for t in (k, v, k_scales, v_scales):
+            if not t.is_contiguous():
+                raise ValueError("the cache's tensors must be contiguous")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.heads, self.head_dim, self.block = heads, dim, block
+        self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), blocks,
+                                  heads, dim, block)
+
+    @classmethod
+    def empty(cls, num_blocks, heads, head_dim, block, device="cuda"):
+        import torch
+        return cls(torch.empty((num_blocks, heads, block, head_dim), dtype=torch.int8, device=device),
+                   torch.empty((num_blocks, heads, head_dim, block), dtype=torch.int8, device=device),
+                   torch.empty((num_blocks, heads), dtype=torch.float32, device=device),
+                   torch.empty((num_blocks, heads), dtype=torch.float32, device=device))
+
+
+class Batch:
+    """The sequences of a call on CUDA int32 tensors: starts (sequences + 1), lengths (sequences) and blocks
+    (sequences x entries, rows with adjacent entries); rows, max_rows and max_length are plain numbers
+    (the rows of the row tensors, and bounds).  Keeps the tensors alive."""
+
+    def __init__(self, starts, lengths, blocks, rows, max_rows, max_length):
+        import torch
+        n = lengths.shape[0]
+        for t in (starts, lengths, blocks):
+            if t.dtype != torch.int32:
+                raise ValueError("starts, lengths and blocks must be int32")
+        if tuple(starts.shape) != (n + 1,) or lengths.dim() != 1 or blocks.dim() != 2 or blocks.shape[0] != n:
+            raise ValueError("starts, lengths and blocks must have sequences + 1, sequences and sequences rows")
+        if not starts.is_contiguous() or not lengths.is_contiguous():
+            raise ValueError("starts and lengths must be contiguous")
+        ld = _rows_2d(blocks, "blocks")
+        self.starts, self.lengths, self.blocks, self.rows = starts, lengths, blocks, rows
+        # the last row holds blocks.shape[1] entries, so no position may lie past them
+        self.entries = blocks.shape[1]
+        self.max_length = max_length
+        self.struct = BatchStruct(n, starts.data_ptr(), lengths.data_ptr(), blocks.data_ptr(), ld, rows, max_rows,
+                                  max_length)
+
+
+def _row_tensor(t, cache, batch, heads, what):
+    if t.dim() != 3 or tuple(t.shape) != (batch.rows, heads, cache.head_dim) or t.stride(2) != 1:
+        raise ValueError("%s must be rows x %d x %d with adjacent elements in the last dimension"
+                         % (what, heads, cache.head_dim))
+    return t.stride(0), t.stride(1)
+
+
+def _fits(cache, batch):
+    if batch.max_length > batch.entries * cache.block:
+        raise ValueError("max_length lies past the block table's entries")
+
+
+def store_tokens(cache, batch, k, v, d_range_flag=None):
+    """Stores k and v (rows x heads x dim) as the newest tokens of the batch's sequences."""
+    _fits(cache, batch)
+    k_row, k_head = _row_tensor(k, cache, batch, cache.heads, "k")
+    v_row, v_head = _row_tensor(v, cache, batch, cache.heads, "v")
+    if k.dtype != v.dtype:
+        raise ValueError("k and v have different types")
+    _on_current_device(cache.k, batch.starts, k, v)
+    cache_store(cache, batch, k, k_row, k_head, v, v_row, v_head, _dtype(k.dtype, (F32, BF16, F16)), d_range_flag)
+
+
+def load_tokens(cache, batch, dtype, d_range_flag=None):
+    """(k, v), rows x heads x dim of dtype: what the newest tokens of the batch's sequences stand for.
+    Rows that belong to no sequence are not written."""
+    import torch
+    _fits(cache, batch)
+    _on_current_device(cache.k, batch.starts)
+    shape = (batch.rows, cache.heads, cache.head_dim)
+    k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
+    row, head = shape[1] * shape[2], shape[2]
+    cache_load(cache, batch, k, row, head, v, row, head, _dtype(dtype, (F32, BF16, F16)), d_range_flag)
+    return k, v
+
+
+def attend(cache, batch, q, scale, causal=True, out=None, d_range_flag=None):
+    """Attention of q (rows x query heads x dim) over the cached tokens of the batch's sequences.  Rows that
+    belong to no sequence are not written."""
+    import torch
+    _fits(cache, batch)
+    heads = q.shape[1] if q.dim() == 3 else 0
+    q_row, q_head = _row_tensor(q, cache, batch, heads, "q")
+    dtype = _dtype(q.dtype, (BF16, F16))
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    elif out.dtype != q.dtype:
+        raise ValueError("out and q have different types")
+    out_row, out_head = _row_tensor(out, cache, batch, heads, "out")
+    _on_current_device(cache.k, batch.starts, q, out)
+    n = cache_attend_workspace_bytes(cache, batch, heads)
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    cache_attend(cache, batch, q, q_row, q_head, heads, dtype, scale, 1 if causal else 0, out, out_row, out_head, ws,
+                 n, d_range_flag)
+    return out
