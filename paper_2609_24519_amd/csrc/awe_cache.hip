@@ -89,59 +89,309 @@ __global__ __launch_bounds__(256) void load_plain_kernel(CacheLaunch g) {
                (float)q[element(g.c, values, t.t0 + e / D, e % D)] * scale);
 }
 
-// One wave per row and query head: 64 tokens at a time, one per lane, for the scores, and the
-// dimensions over the lanes for the values; running maximum and sum.
-__global__ __launch_bounds__(64) void attend_plain_kernel(AttendLaunch g) {
-  const int lane = threadIdx.x, D = g.c.head_dim, qh = blockIdx.y, head = qh / (g.q_heads / g.c.heads);
-  const Seq s = sequence(g.b, blockIdx.z, false, g.flag, lane == 0);
-  __shared__ float qs[256], ps[64];
-  for (int32_t i = blockIdx.x; i < s.rows; i += gridDim.x) {
-    __syncthreads();
-    for (int d = lane; d < D; d += 64)
-      qs[d] = load_real(g.q.p, (int64_t)(s.row0 + i) * g.q.row + qh * g.q.head + d, g.type);
-    __syncthreads();
-    const int32_t keys = g.causal ? s.len - s.rows + i + 1 : s.len;
-    float m = -INFINITY, l = 0.f, o[4] = {};
-    for (int32_t j0 = 0; j0 < keys; j0 += 64) {
-      const int32_t j = j0 + lane;
-      const int32_t id = j < keys ? block_of(g.c, g.b, blockIdx.z, j, g.flag) : -1;
-      const int64_t at = (int64_t)id * g.c.heads + head;
-      float score = -INFINITY;
-      if (id >= 0) {
-        const int8_t* k = g.c.k + at * g.c.block * D + element(g.c, false, j % g.c.block, 0);
-        float dot = 0.f;
-        for (int d = 0; d < D; ++d) dot += qs[d] * (float)k[d];
-        score = dot * g.c.k_scales[at] * g.scale;
+// ---- attention ------------------------------------------------------------------------------
+// A wave works on 16-column tiles: column c of a sequence's cache head is row c / share with query head
+// c % share of that head's group.  Tokens come 64 at a time, four chunks of 16 that each lie in one block:
+//   S^T (tokens x columns) = K Q^T,  P = exp2(S - running maximum),  O^T (dimensions x columns) = V^T P^T,
+// both on the 16x16x32 FP16 MFMA.  Lane 16 q + i holds, of the operands, row (token or dimension) i or
+// column i at the reduction indices of quarter q, and of a result, column i at rows 4 q .. 4 q + 3.
+// The order of tokens and dimensions along a reduction and of the rows of S^T is free, so it is taken such that nothing
+// moves between lanes and every load is 16 bytes: row i of S^T's tile t is token 16 (i / 4) + 4 t + i % 4, so
+// lane (q, i) gets the scores of tokens 16 q .. 16 q + 15, which are its part of P^T, and it loads the same
+// 16 tokens of dimension i from V, 16 adjacent bytes as V is kept by dimension.
+// int8 becomes FP16 exactly (a byte permute into 1024 + u, less 1152).  Queries become FP16 by a power
+// of two per column that brings the largest below 2^15: what that loses lies 2^-40 below the largest.
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr int kWaves = 4;     // per workgroup
+constexpr int kTokens = 64;   // per step of a wave
+constexpr float kLog2e = 1.4426950408889634f;
+
+union Halves {
+  h8 v;
+  h2 p[4];
+  uint32_t w[4];
+};
+
+// Eight int8 (two words) as FP16.
+__device__ __forceinline__ h8 widen(uint32_t a, uint32_t b) {
+  Halves r;
+  const h2 less = {(_Float16)-1152.f, (_Float16)-1152.f};
+  a ^= 0x80808080u;
+  b ^= 0x80808080u;
+  r.w[0] = __builtin_amdgcn_perm(0x64646464u, a, 0x04010400u);
+  r.w[1] = __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u);
+  r.w[2] = __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u);
+  r.w[3] = __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.p[i] += less;
+  return r.v;
+}
+
+// Largest over the four quarters of a column (NaN is passed over; it shows in the sum).
+__device__ __forceinline__ float quarters_max(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+struct AttendArgs {
+  AttendLaunch g;
+  int32_t share, log2_block;
+  int32_t chunk;       // tokens of a workgroup (kSplit), a multiple of kWaves * kTokens
+  int32_t splits;      // workgroups per sequence, head and column tile
+  int32_t col_groups;  // column groups (workgroups along the columns) that max_rows asks for
+  float* part;         // workspace: kPart(D) floats per column and split
+};
+
+// Partial results of column c (of sequence s, head h) and split x: maximum, sum, and D values.
+__device__ __forceinline__ int64_t part_index(const AttendArgs& a, int s, int h, int64_t c, int x, int D) {
+  const int64_t cols = (int64_t)a.g.b.max_rows * a.share;
+  return ((((int64_t)s * a.g.c.heads + h) * cols + c) * a.splits + x) * (D + 4);
+}
+
+// kSplit: a workgroup has 16 kQ columns and a chunk of the tokens, which its waves take 64 at a time
+// in turn; otherwise its waves have 16 kQ columns each and all of the tokens.
+template <int D, int kQ, bool kSplit>
+__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
+  const awe_cache& c = a.g.c;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
+  const int sid = blockIdx.z, head = blockIdx.y;
+  const int group = kSplit ? blockIdx.x / a.splits : blockIdx.x, split = kSplit ? blockIdx.x % a.splits : 0;
+  const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && blockIdx.x == 0);
+  const int64_t cols = (int64_t)s.rows * a.share;
+  const int64_t col0 = (kSplit ? group : (int64_t)group * kWaves + wave) * 16 * kQ;
+  if (kSplit ? col0 >= cols : (int64_t)group * kWaves * 16 * kQ >= cols) return;
+  // tokens of this workgroup; a sequence without any is one empty chunk
+  const int32_t from = kSplit ? split * a.chunk : 0;
+  if (kSplit && split > 0 && from >= s.len) return;
+  int32_t to = kSplit && s.len - from > a.chunk ? from + a.chunk : s.len;
+
+  // the columns: how many tokens each sees, and its query
+  int32_t last[kQ];
+  float factor[kQ];
+  h8 qf[kQ][D / 32];
+#pragma unroll
+  for (int t = 0; t < kQ; ++t) {
+    const int64_t col = col0 + 16 * t + i16;
+    const bool ok = col < cols;
+    const int32_t row = ok ? (int32_t)(col / a.share) : 0;
+    last[t] = !ok ? 0 : a.g.causal ? s.len - s.rows + row + 1 : s.len;
+    const int64_t at = (int64_t)(s.row0 + row) * a.g.q.row + (int64_t)(head * a.share + (ok ? col % a.share : 0)) * a.g.q.head;
+    float v[D / 32][8];
+    float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int d = 64 * (j >> 1) + 16 * q4 + 8 * (j & 1) + e;
+        v[j][e] = ok ? load_real(a.g.q.p, at + d, a.g.type) : 0.f;
+        most = fmaxf(most, fabsf(v[j][e]));
       }
-      float top = score;
-      for (int d = 32; d > 0; d >>= 1) {
-        const float other = __shfl_xor(top, d);
-        top = other > top || other != other ? other : top;
+    most = quarters_max(most);
+    const int ex = most > 0.f ? __builtin_amdgcn_frexp_expf(most) : 0;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) qf[t][j][e] = (_Float16)ldexpf(v[j][e], 15 - ex);
+    factor[t] = ldexpf(a.g.scale * kLog2e, ex - 15);
+  }
+  if (!kSplit && a.g.causal) {
+    // the last column's row sees the most tokens
+    const int64_t end = col0 + 16 * kQ < cols ? col0 + 16 * kQ : cols;
+    const int32_t most = end > col0 ? s.len - s.rows + (int32_t)((end - 1) / a.share) + 1 : 0;
+    to = most < to ? most : to;
+  }
+  if (!kSplit && col0 >= cols) to = 0;
+
+  f4 o[kQ][D / 16];
+  float m[kQ], l[kQ];
+  int ev[kQ];  // exponent that brings the values' scales seen so far below 1
+#pragma unroll
+  for (int t = 0; t < kQ; ++t) {
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+    ev[t] = -1000;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) o[t][d] = f4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int64_t tile = (int64_t)c.block * D;
+  const int chunk_k = i16 >> 2;
+  const int32_t step = kSplit ? kWaves * kTokens : kTokens;
+  for (int32_t t0 = from + (kSplit ? wave * kTokens : 0); t0 < to; t0 += step) {
+    // the blocks of this lane's chunk of keys and chunk of values (-1: past the end, or a bad id)
+    const int32_t pk = t0 + 16 * chunk_k, pv = t0 + 16 * q4;
+    const int32_t ik = pk < s.len ? block_of(c, a.g.b, sid, pk, nullptr) : -1;
+    const int32_t iv = pv < s.len ? block_of(c, a.g.b, sid, pv, a.g.flag) : -1;
+    const int64_t ak = ((int64_t)ik * c.heads + head), av = ((int64_t)iv * c.heads + head);
+    u4 kr[4][D / 64], vr[D / 16];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d)
+        kr[t][d] = ik < 0 ? u4{0, 0, 0, 0}
+                          : *reinterpret_cast<const u4*>(c.k + ak * tile + ((pk & (c.block - 1)) + 4 * t + (i16 & 3)) * D + 64 * d + 16 * q4);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+      vr[d] = iv < 0 ? u4{0, 0, 0, 0}
+                     : *reinterpret_cast<const u4*>(c.v + av * tile + (16 * d + i16) * c.block + (pv & (c.block - 1)));
+    const float ks = iv < 0 ? 0.f : c.k_scales[av], vs = iv < 0 ? 0.f : c.v_scales[av];
+
+    f4 sc[kQ][4];
+#pragma unroll
+    for (int t = 0; t < kQ; ++t)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) sc[t][b] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const h8 kf = widen(kr[b][j >> 1][2 * (j & 1)], kr[b][j >> 1][2 * (j & 1) + 1]);
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][j], sc[t][b], 0, 0, 0);
       }
-      if (top == -INFINITY) continue;
-      const float now = top > m || top != top ? top : m, keep = m == -INFINITY ? 0.f : expf(m - now);
-      const float p = score == -INFINITY ? 0.f : expf(score - now);
-      m = now;
-      float sum = p;
-      for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-      l = l * keep + sum;
-      ps[lane] = p;
+
+    // softmax of the lane's 16 tokens of its column, against the running maximum
+    int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
+    et = max(et, __shfl_xor(et, 16));
+    et = max(et, __shfl_xor(et, 32));
+    h8 pf[kQ][2];
+#pragma unroll
+    for (int t = 0; t < kQ; ++t) {
+      const float f = factor[t] * ks;
+      float top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool see = iv >= 0 && pv + 4 * b + r < last[t];
+          sc[t][b][r] = see ? sc[t][b][r] * f : -INFINITY;
+          top = fmaxf(top, sc[t][b][r]);
+        }
+      const float now = fmaxf(m[t], quarters_max(top));
+      const float base = now == -INFINITY ? 0.f : now;
+      const int e = max(ev[t], et);
+      const float keep = ldexpf(__builtin_amdgcn_exp2f(m[t] - base), ev[t] - e);
+      l[t] *= __builtin_amdgcn_exp2f(m[t] - base);
+      m[t] = now;
+      ev[t] = e;
+      // a weight times its block's scale, below 2^15 times the largest scale so far: FP16 keeps
+      // 11 bits of what is at least 2^-29 of the largest, and to 2^-40 of it of the rest
+      const float w = ldexpf(vs, 15 - e);
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float p = __builtin_amdgcn_exp2f(sc[t][b][r] - base);
+          l[t] += p;
+          pf[t][b >> 1][4 * (b & 1) + r] = (_Float16)(p * w);
+        }
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[t][d] *= keep;
+    }
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const h8 vf = widen(vr[d][2 * e], vr[d][2 * e + 1]);
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][e], o[t][d], 0, 0, 0);
+      }
+  }
+#pragma unroll
+  for (int t = 0; t < kQ; ++t) {
+    l[t] += __shfl_xor(l[t], 16);
+    l[t] += __shfl_xor(l[t], 32);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r], ev[t] - 15);
+  }
+
+  if (!kSplit) {
+#pragma unroll
+    for (int t = 0; t < kQ; ++t) {
+      const int64_t col = col0 + 16 * t + i16;
+      if (col >= cols) continue;
+      const int64_t at = (int64_t)(s.row0 + col / a.share) * a.g.o.row + (head * a.share + col % a.share) * a.g.o.head;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          store_real(a.g.o.p, at + 16 * d + 4 * q4 + r, a.g.type, l[t] == 0.f ? 0.f : o[t][d][r] / l[t]);
+    }
+    return;
+  }
+  // the waves' parts of each column, through LDS: 64 dimensions at a time
+  constexpr int kDim = 64;
+  __shared__ float ow[kWaves][16][kDim + 4], mw[kWaves][16], lw[kWaves][16];
+  const bool whole = s.len <= a.chunk;
+#pragma unroll
+  for (int t = 0; t < kQ; ++t) {
+#pragma unroll
+    for (int d0 = 0; d0 < D; d0 += kDim) {
       __syncthreads();
-      for (int a = 0; a < D / 64; ++a) {
-        o[a] *= keep;
-        for (int t = 0; t < 64; ++t) {
-          const int32_t id_t = __shfl(id, t);
-          if (id_t < 0) continue;
-          const int64_t at_t = (int64_t)id_t * g.c.heads + head;
-          const float v = (float)g.c.v[at_t * g.c.block * D + element(g.c, true, (j0 + t) % g.c.block, a * 64 + lane)];
-          o[a] += ps[t] * v * g.c.v_scales[at_t];
+      if (q4 == 0 && d0 == 0) {
+        mw[wave][i16] = m[t];
+        lw[wave][i16] = l[t];
+      }
+#pragma unroll
+      for (int d = 0; d < kDim / 16; ++d) *reinterpret_cast<f4*>(&ow[wave][i16][16 * d + 4 * q4]) = o[t][d0 / 16 + d];
+      __syncthreads();
+      // thread: column threadIdx / 16, four dimensions
+      const int cl = threadIdx.x >> 4, d = 4 * (threadIdx.x & 15);
+      const int64_t col = col0 + 16 * t + cl;
+      float top = -INFINITY, sum = 0.f;
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mw[w][cl]);
+      f4 v = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(mw[w][cl] - (top == -INFINITY ? 0.f : top));
+        sum += lw[w][cl] * f;
+        v += *reinterpret_cast<const f4*>(&ow[w][cl][d]) * f;
+      }
+      if (col >= cols) continue;
+      if (whole) {
+        const int64_t at = (int64_t)(s.row0 + col / a.share) * a.g.o.row + (head * a.share + col % a.share) * a.g.o.head;
+        for (int r = 0; r < 4; ++r) store_real(a.g.o.p, at + d0 + d + r, a.g.type, sum == 0.f ? 0.f : v[r] / sum);
+      } else {
+        float* p = a.part + part_index(a, sid, head, col, split, D);
+        *reinterpret_cast<f4*>(p + 4 + d0 + d) = v;
+        if (d0 == 0 && d == 0) {
+          p[0] = top;
+          p[1] = sum;
         }
       }
-      __syncthreads();
     }
-    for (int a = 0; a < D / 64; ++a)
-      store_real(g.o.p, (int64_t)(s.row0 + i) * g.o.row + qh * g.o.head + a * 64 + lane, g.type, l == 0.f ? 0.f : o[a] / l);
   }
+}
+
+// Joins the splits of a column: 64 threads per column, D / 64 dimensions each.
+template <int D>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
+  const int sid = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63;
+  const Seq s = sequence(a.g.b, sid, false, nullptr, false);
+  const int64_t col = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (s.len <= a.chunk || col >= (int64_t)s.rows * a.share) return;
+  const int n = (s.len + a.chunk - 1) / a.chunk;
+  const float* p = a.part + part_index(a, sid, head, col, 0, D);
+  float top = -INFINITY, sum = 0.f, v[D / 64] = {};
+  for (int x = lane; x < n; x += 64) top = fmaxf(top, p[(int64_t)x * (D + 4)]);
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+  for (int x = 0; x < n; ++x) {
+    const float* px = p + (int64_t)x * (D + 4);
+    const float f = __builtin_amdgcn_exp2f(px[0] - base);
+    sum += px[1] * f;
+#pragma unroll
+    for (int d = 0; d < D / 64; ++d) v[d] += px[4 + 64 * d + lane] * f;
+  }
+  const int64_t at = (int64_t)(s.row0 + col / a.share) * a.g.o.row + (head * a.share + col % a.share) * a.g.o.head;
+#pragma unroll
+  for (int d = 0; d < D / 64; ++d) store_real(a.g.o.p, at + 64 * d + lane, a.g.type, sum == 0.f ? 0.f : v[d] / sum);
 }
 
 // Grid (blocks that can be touched, heads, 2 * sequences); sequences go over in parts of the grid's limit.
@@ -172,17 +422,43 @@ awe_status launch_cache_load(const CacheLaunch& g, hipStream_t stream) {
   return launch_tiles(load_plain_kernel, g, "cache load launch", stream);
 }
 
+namespace {
+template <int D>
+awe_status launch_attend(const AttendArgs& a, int columns, hipStream_t stream) {
+  const dim3 block(64 * kWaves);
+  const unsigned heads = (unsigned)a.g.c.heads, seqs = (unsigned)a.g.b.sequences;
+  if (columns > 0) {
+    hipLaunchKernelGGL((attend_kernel<D, 2, false>), dim3((unsigned)a.col_groups, heads, seqs), block, 0, stream, a);
+    return launched("attention launch");
+  }
+  hipLaunchKernelGGL((attend_kernel<D, 1, true>), dim3((unsigned)(a.col_groups * a.splits), heads, seqs), block, 0, stream, a);
+  awe_status st = launched("attention launch");
+  if (st != AWE_OK || a.splits == 1) return st;
+  const int64_t cols = a.g.b.max_rows * a.share;
+  hipLaunchKernelGGL((attend_join_kernel<D>), dim3((unsigned)((cols + 3) / 4), heads, seqs), dim3(256), 0, stream, a);
+  return launched("attention join launch");
+}
+}  // namespace
+
 awe_status launch_cache_attend(const AttendLaunch& g, hipStream_t stream) {
-  const unsigned x = (unsigned)(g.b.max_rows < 4096 ? g.b.max_rows : 4096);
+  const AttendPlan plan = plan_attend(g.c, g.b, g.q_heads);
+  // sequences go over in parts of the grid's limit
   for (int32_t s = 0; s < g.b.sequences; s += 65535) {
-    AttendLaunch part = g;
-    part.b.sequences = g.b.sequences - s < 65535 ? g.b.sequences - s : 65535;
-    part.b.starts += s;
-    part.b.lengths += s;
-    part.b.blocks += s * g.b.ld_blocks;
-    hipLaunchKernelGGL(attend_plain_kernel, dim3(x, (unsigned)g.q_heads, (unsigned)part.b.sequences), dim3(64), 0,
-                       stream, part);
-    const awe_status st = launched("attention launch");
+    AttendArgs a{};
+    a.g = g;
+    a.g.b.sequences = g.b.sequences - s < 65535 ? g.b.sequences - s : 65535;
+    a.g.b.starts += s;
+    a.g.b.lengths += s;
+    a.g.b.blocks += s * g.b.ld_blocks;
+    if (a.g.b.max_rows > a.g.b.rows) a.g.b.max_rows = a.g.b.rows;
+    a.share = g.q_heads / g.c.heads;
+    a.chunk = plan.chunk;
+    a.splits = plan.splits;
+    a.col_groups = plan.groups;
+    a.part = reinterpret_cast<float*>(g.ws);
+    const awe_status st = g.c.head_dim == 64    ? launch_attend<64>(a, plan.own_columns, stream)
+                          : g.c.head_dim == 128 ? launch_attend<128>(a, plan.own_columns, stream)
+                                                : launch_attend<256>(a, plan.own_columns, stream);
     if (st != AWE_OK) return st;
   }
   return AWE_OK;

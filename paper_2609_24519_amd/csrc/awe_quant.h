@@ -54,7 +54,15 @@ struct AttendLaunch {
   int32_t* flag;
 };
 awe_status launch_cache_attend(const AttendLaunch& g, hipStream_t stream);
-// Workspace of a call, from its host-side sizes alone (0: no sequence is split).
-size_t attend_workspace(const awe_cache& c, const awe_batch& b, int32_t q_heads);
+// How a call is laid over workgroups, from its host-side sizes alone.
+struct AttendPlan {
+  bool own_columns;  // a wave has columns of its own and sees all tokens; otherwise a workgroup's waves share
+                     // 16 columns and split the tokens
+  int32_t groups;    // workgroups along the columns
+  int32_t splits;    // workgroups along the tokens
+  int32_t chunk;     // tokens of each
+  size_t workspace;
+};
+AttendPlan plan_attend(const awe_cache& c, const awe_batch& b, int32_t q_heads);
 
 }  // namespace awe

@@ -1,6 +1,8 @@
 // The C ABI of quantised inference (include/awe.h): argument checks on the host, then the launches.
 #include "awe_quant.h"
 
+#include <algorithm>
+
 namespace awe {
 namespace {
 
@@ -142,7 +144,8 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
   if (st == AWE_OK) st = check_rows(o, type);
   if (st != AWE_OK) return st;
   if (!distinct(o, batch->rows, q_heads, cache->head_dim)) return invalid("written elements share memory");
-  const size_t need = attend_workspace(*cache, *batch, q_heads);
+  if (std::min(batch->rows, batch->max_rows) * q_heads > (int64_t(1) << 30)) return refuse(AWE_ERR_UNSUPPORTED, "too many rows");
+  const size_t need = plan_attend(*cache, *batch, q_heads).workspace;
   if (need > 0 && (ws == nullptr || ws_bytes < need))
     return refuse(AWE_ERR_WORKSPACE, "workspace smaller than awe_cache_attend_workspace_bytes");
   if (need > 0 && !aligned(ws, 16)) return invalid("workspace must be aligned to 16 bytes");
@@ -152,7 +155,28 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
 
 }  // namespace
 
-size_t attend_workspace(const awe_cache&, const awe_batch&, int32_t) { return 0; }
+AttendPlan plan_attend(const awe_cache& c, const awe_batch& b, int32_t q_heads) {
+  constexpr int64_t kFill = 2048;   // workgroups that keep the chip busy to the end of ragged sequences
+  constexpr int64_t kChunk = 512;   // fewest tokens worth a workgroup of their own
+  const int64_t rows = std::min(b.max_rows, b.rows);
+  const int64_t cols = rows * (q_heads / c.heads);
+  AttendPlan p{};
+  p.own_columns = cols > 32;
+  p.splits = 1;
+  if (p.own_columns) {
+    p.groups = (int32_t)((cols + 127) / 128);
+    return p;
+  }
+  p.groups = (int32_t)((cols + 15) / 16);
+  const int64_t base = (int64_t)b.sequences * c.heads * p.groups;
+  const int64_t most = std::max<int64_t>(1, (b.max_length + kChunk - 1) / kChunk);
+  const int64_t want = std::min(most, std::max<int64_t>(1, (kFill + base - 1) / std::max<int64_t>(base, 1)));
+  const int64_t chunk = ((b.max_length + want - 1) / want + 255) / 256 * 256;
+  p.chunk = (int32_t)std::max<int64_t>(chunk, 256);
+  p.splits = (int32_t)std::max<int64_t>(1, (b.max_length + p.chunk - 1) / p.chunk);
+  if (p.splits > 1) p.workspace = (size_t)b.sequences * c.heads * cols * p.splits * (c.head_dim + 4) * sizeof(float);
+  return p;
+}
 
 }  // namespace awe
 
@@ -190,7 +214,7 @@ awe_status awe_cache_attend_workspace_bytes(const awe_cache* cache, const awe_ba
     awe_status st = check_cache(cache);
     if (st == AWE_OK) st = check_batch(*cache, batch);
     if (st == AWE_OK) st = check_heads(*cache, q_heads);
-    if (st == AWE_OK) *bytes = empty(*batch) ? 0 : attend_workspace(*cache, *batch, q_heads);
+    if (st == AWE_OK) *bytes = empty(*batch) ? 0 : plan_attend(*cache, *batch, q_heads).workspace;
     return st;
   });
 }
