@@ -117,37 +117,6 @@ __device__ __forceinline__ typename Kind<T>::Raw load8(const typename Kind<T>::E
     return u4{a.w[0], a.w[1], a.w[2], a.w[3]};
   }
 }
-// The first n of them (0 for the rest): a load each for the bits of n.
-struct __attribute__((packed)) Any4 {
-  uint32_t w;
-};
-struct __attribute__((packed)) Any2 {
-  uint16_t w;
-};
-template <awe_dtype T>
-__device__ __forceinline__ typename Kind<T>::Raw load8_short(const typename Kind<T>::Elem* p, int n) {
-  if (n >= 8) return load8<T>(p);
-  uint64_t lo = 0, hi = 0;
-  const int at2 = n & 4, at1 = n & 6;  // where the pair and the last one lie
-  if constexpr (T == AWE_I8) {
-    if (n > 0) {
-      if (n & 4) lo = reinterpret_cast<const Any4*>(p)->w;
-      if (n & 2) lo |= (uint64_t)reinterpret_cast<const Any2*>(p + at2)->w << (8 * at2);
-      if (n & 1) lo |= (uint64_t)p[at1] << (8 * at1);
-    }
-    return lo;
-  } else {
-    if (n > 0) {
-      if (n & 4) {
-        const Any8 v = *reinterpret_cast<const Any8*>(p);
-        lo = (uint64_t)v.w[0] | (uint64_t)v.w[1] << 32;
-      }
-      if (n & 2) (at2 ? hi : lo) |= reinterpret_cast<const Any4*>(p + at2)->w;
-      if (n & 1) (at1 & 4 ? hi : lo) |= (uint64_t)p[at1] << (16 * (at1 & 2));
-    }
-    return u4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-  }
-}
 template <awe_dtype T>
 __device__ __forceinline__ typename Kind<T>::Raw none() {
   return typename Kind<T>::Raw{};
@@ -166,7 +135,8 @@ constexpr int kChunk = 128;  // reduction indices of a wave's step: 16 bytes of 
 
 struct W4Args {
   W4Launch g;
-  int32_t units;  // group / 128, or group / 32 where 128 does not divide it
+  int32_t units;           // group / 128, or group / 32 where 128 does not divide it
+  int32_t step_g, step_u;  // 8 chunks are step_g groups and step_u units
 };
 
 // The chunk of a lane: row n of W at indices 32 q .. 32 q + 31 of the chunk.  kFine: a group may begin at any
@@ -178,13 +148,31 @@ __device__ __forceinline__ int step_offset(int q, int j) {
   return kFine ? 32 * j + 8 * q : 32 * q + 8 * j;
 }
 
+// A scale as it lies in memory, and its value.
+template <bool kS4>
+__device__ __forceinline__ uint32_t raw_scale(const void* p, int64_t i) {
+  if constexpr (kS4)
+    return reinterpret_cast<const uint32_t*>(p)[i];
+  else
+    return reinterpret_cast<const uint16_t*>(p)[i];
+}
+template <bool kS4>
+__device__ __forceinline__ float scale_value(uint32_t raw, bool is_bf16) {
+  if constexpr (kS4) return __builtin_bit_cast(float, raw);
+  const float h = (float)__builtin_bit_cast(_Float16, (uint16_t)raw);
+  return is_bf16 ? __builtin_bit_cast(float, raw << 16) : h;
+}
+
 // Few rows: 16 outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
 // with kM x 16 rows of X; operands go straight from memory to the matrix unit.  Bound by the
-// weights' bytes: a wave has kU chunks of them in flight.
-template <awe_dtype T, int kM, bool kFine>
-__global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
+// weights' bytes: a wave has kD chunks of them in flight, and the rows of one chunk ahead.
+constexpr int kW = 8;
+template <awe_dtype T, int kM, bool kFine, bool kS4>
+__global__ __launch_bounds__(64 * kW, kM == 1 ? 4 : 2) void w4_rows_kernel(W4Args a) {
   using X = Kind<T>;
-  constexpr int kW = 8, kU = kM == 1 ? 4 : kM == 2 ? 2 : 1;
+  constexpr int kD = kFine ? 2 : (kM == 1 ? 8 : 4);   // chunks of W in flight
+  constexpr int kX = kFine && kM == 4 ? 1 : 2;          // chunks of X (kD is a multiple)
+  constexpr int kS = kFine ? 4 : 1;
   const W4Launch& g = a.g;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
   const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16 * kM;
@@ -197,20 +185,23 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
     ok[t] = m0 + 16 * t + i < g.M;
     x[t] = reinterpret_cast<const typename X::Elem*>(g.x) + (ok[t] ? m0 + 16 * t + i : 0) * g.ldx;
   }
+  const bool is_bf16 = g.s_type == AWE_BF16, has_z = g.zeros != nullptr;
+  const int64_t s0 = n * g.lds, z0 = n * g.ldz;
+  const uint8_t* zp = has_z ? g.zeros : g.w;  // (any byte, where there are none)
   const uint32_t magic = X::magic();
   f4 acc[kM];
 #pragma unroll
   for (int t = 0; t < kM; ++t) acc[t] = f4{0.f, 0.f, 0.f, 0.f};
 
   // adds a group's part: part - (bias + z) sum x, times the group's scale
-  auto fold = [&](const typename X::Acc* part, const typename X::Acc* sum, float s, float z) {
-    const float b = X::kBias + z;
+  auto fold = [&](const typename X::Acc* part, const typename X::Acc* sum, uint32_t rs, uint32_t rz) {
+    const float s = scale_value<kS4>(rs, is_bf16), b = X::kBias + (has_z ? (float)rz : 8.f);
 #pragma unroll
     for (int t = 0; t < kM; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) acc[t][r] += s * ((float)part[t][r] - b * (float)sum[t][r]);
   };
-  auto chunk = [&](u4 cw, const typename X::Raw (&xr)[kM][4], const float* s, const float* z) {
+  auto chunk = [&](u4 cw, const typename X::Raw (&xr)[kM][4], const uint32_t* s, const uint32_t* z) {
     typename X::Acc part[kM], sum[kM];
     if (kFine) cw = across_quarters(cw);
 #pragma unroll
@@ -226,91 +217,147 @@ __global__ __launch_bounds__(512) void w4_rows_kernel(W4Args a) {
       if (kFine || j == 3) fold(part, sum, s[kFine ? j : 0], z[kFine ? j : 0]);
     }
   };
-  // scale and zero point of lane's output in the group of unit u (128 or 32 indices)
-  constexpr int kS = kFine ? 4 : 1;
-  auto scales = [&](int32_t c, float* s, float* z, int units) {
+  // Scales and zero points of the lane's output in the groups of a chunk whose first unit is unit `u` of
+  // group `grp`; groups past `last` are not touched.
+  auto scales = [&](int32_t grp, int32_t u, int32_t last, uint32_t* s, uint32_t* z) {
 #pragma unroll
     for (int j = 0; j < kS; ++j) {
-      const int32_t grp = (uint32_t)(kFine ? 4 * c + (j < units ? j : 0) : c) / (uint32_t)a.units;
-      s[j] = load_real(g.scales, n * g.lds + grp, g.s_type);
-      z[j] = g.zeros != nullptr ? (float)g.zeros[n * g.ldz + grp] : 8.f;
+      const int32_t at = grp < last ? grp : last;
+      s[j] = raw_scale<kS4>(g.scales, s0 + at);
+      z[j] = zp[has_z ? z0 + at : 0];
+      if (++u == a.units) u = 0, ++grp;
+    }
+  };
+  auto codes = [&](int32_t c) {
+    const Any16 v = *reinterpret_cast<const Any16*>(w + (int64_t)c * (kChunk / 2));
+    return u4{v.w[0], v.w[1], v.w[2], v.w[3]};
+  };
+  auto rows = [&](int32_t c, typename X::Raw (&xr)[kM][4]) {
+#pragma unroll
+    for (int t = 0; t < kM; ++t) {
+      const typename X::Elem* p = x[t] + (int64_t)c * kChunk;
+      if constexpr (T == AWE_I8 && !kFine) {
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const u4 v = ok[t] ? load8<AWE_BF16>(reinterpret_cast<const uint16_t*>(p + step_offset<kFine>(q, j))) : u4{0, 0, 0, 0};
+          xr[t][j] = (uint64_t)v[0] | (uint64_t)v[1] << 32;
+          xr[t][j + 1] = (uint64_t)v[2] | (uint64_t)v[3] << 32;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) xr[t][j] = ok[t] ? load8<T>(p + step_offset<kFine>(q, j)) : none<T>();
+      }
     }
   };
 
+  // chunk wave + 8 t begins in unit `unit` of group `grp` (ahead: of the chunk that is fetched next)
   const int32_t full = (int32_t)(g.K / kChunk);
-  for (int32_t c0 = wave; c0 < full; c0 += kW * kU) {
-    u4 cw[kU];
-    typename X::Raw xr[kU][kM][4];
-    float s[kU][kS], z[kU][kS];
+  const uint32_t first_unit = (uint32_t)wave * (kFine ? 4 : 1);
+  int32_t grp = (int32_t)(first_unit / (uint32_t)a.units), unit = (int32_t)(first_unit % (uint32_t)a.units);
+  auto next = [&] {
+    grp += a.step_g;
+    unit += a.step_u;
+    if (unit >= a.units) unit -= a.units, ++grp;
+  };
+  const int32_t last = (int32_t)((g.K - 1) / g.group);
+  if (wave < full) {
+    u4 cw[kD];
+    typename X::Raw xr[kX][kM][4];
+    uint32_t s[kD][kS], z[kD][kS];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int32_t c = c0 + u * kW;
-      if (c < full) {
-        const Any16 v = *reinterpret_cast<const Any16*>(w + (int64_t)c * (kChunk / 2));
-        cw[u] = u4{v.w[0], v.w[1], v.w[2], v.w[3]};
+    for (int u = 0; u < kD; ++u) {  // (past the end: the last chunk again, unused)
+      const int32_t c = wave + u * kW;
+      cw[u] = codes(c < full ? c : full - 1);
+      scales(grp, unit, last, s[u], z[u]);
+      next();
+    }
+    if (kX == 2) rows(wave, xr[0]);
+    for (int32_t c0 = wave; c0 < full; c0 += kW * kD) {
+#pragma unroll
+      for (int u = 0; u < kD; ++u) {
+        const int32_t c = c0 + u * kW;
+        if (c >= full) break;
+        if (kX == 2)
+          rows(c + kW < full ? c + kW : full - 1, xr[(u + 1) % kX]);
+        else
+          rows(c, xr[0]);
+        chunk(cw[u], xr[u % kX], s[u], z[u]);
+        const int32_t ahead = c + kW * kD;
+        if (ahead < full) {
+          cw[u] = codes(ahead);
+          scales(grp, unit, last, s[u], z[u]);
+          next();
+        }
       }
     }
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int32_t c = c0 + u * kW;
-      if (c < full) {
-#pragma unroll
-        for (int t = 0; t < kM; ++t)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            xr[u][t][j] = ok[t] ? load8<T>(x[t] + (int64_t)c * kChunk + step_offset<kFine>(q, j)) : none<T>();
-        scales(c, s[u], z[u], 4);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kU; ++u)
-      if (c0 + u * kW < full) chunk(cw[u], xr[u], s[u], z[u]);
   }
-  // the last, short chunk
-  if ((int64_t)full * kChunk < g.K && full % kW == wave) {
+  // the last, short chunk, filled up with zeros in LDS
+  __shared__ union {
+    float red[kW][16 * kM][17];
+    struct {
+      alignas(16) uint8_t w[16][kChunk / 2];
+      alignas(16) typename X::Elem x[16 * kM][kChunk];
+    } end;
+  } lds;
+  if ((int64_t)full * kChunk < g.K) {
     const int64_t k0 = (int64_t)full * kChunk;
-    const int left = (int)(g.K - k0), bytes = (left + 1) / 2 - 16 * q;
-    u4 cw = {0, 0, 0, 0};
-    const uint8_t* p = w + k0 / 2;
+    const int left = (int)(g.K - k0);
+    for (int e = threadIdx.x; e < 16 * (kChunk / 2); e += 64 * kW) {
+      const int64_t row = n0 + e / (kChunk / 2);
+      const int b = e % (kChunk / 2);
+      lds.end.w[e / (kChunk / 2)][b] = row < g.N && 2 * b < left ? g.w[row * g.ldw + k0 / 2 + b] : 0;
+    }
+    for (int e = threadIdx.x; e < 16 * kM * kChunk; e += 64 * kW) {
+      const int64_t row = m0 + e / kChunk;
+      const int k = e % kChunk;
+      lds.end.x[e / kChunk][k] =
+          row < g.M && k < left ? reinterpret_cast<const typename X::Elem*>(g.x)[row * g.ldx + k0 + k] : 0;
+    }
+    __syncthreads();
+    if (full % kW == wave) {
+      const u4 cw = *reinterpret_cast<const u4*>(&lds.end.w[i][16 * q]);
+      typename X::Raw xr[kM][4];
 #pragma unroll
-    for (int b = 0; b < 16; ++b) cw[b >> 2] |= (b < bytes ? (uint32_t)p[b] : 0u) << (8 * (b & 3));
-    typename X::Raw xr[kM][4];
+      for (int t = 0; t < kM; ++t)
 #pragma unroll
-    for (int t = 0; t < kM; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int off = step_offset<kFine>(q, j);
-        xr[t][j] = load8_short<T>(x[t] + k0 + off, ok[t] ? left - off : 0);
-      }
-    float s[kS], z[kS];
-    scales(full, s, z, (left + 31) / 32);
-    chunk(cw, xr, s, z);
+        for (int j = 0; j < 4; ++j)
+          xr[t][j] = *reinterpret_cast<const typename X::Raw*>(&lds.end.x[16 * t + i][step_offset<kFine>(q, j)]);
+      uint32_t s[kS], z[kS];
+      const uint32_t u0 = (uint32_t)full * (kFine ? 4 : 1);
+      scales((int32_t)(u0 / (uint32_t)a.units), (int32_t)(u0 % (uint32_t)a.units), last, s, z);
+      chunk(cw, xr, s, z);
+    }
+    __syncthreads();
   }
 
   // the waves' sums, and Y
-  __shared__ float red[kW][16 * kM][17];
 #pragma unroll
   for (int t = 0; t < kM; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) red[wave][16 * t + 4 * q + r][i] = acc[t][r];
+    for (int r = 0; r < 4; ++r) lds.red[wave][16 * t + 4 * q + r][i] = acc[t][r];
   __syncthreads();
-  for (int e = threadIdx.x; e < 256 * kM; e += 512) {
+  for (int e = threadIdx.x; e < 256 * kM; e += 64 * kW) {
     const int64_t m = m0 + (e >> 4), j = n0 + (e & 15);
     if (m >= g.M || j >= g.N) continue;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kW; ++k) v += red[k][e >> 4][e & 15];
+    for (int k = 0; k < kW; ++k) v += lds.red[k][e >> 4][e & 15];
     store_real(g.y, m * g.ldy + j, g.y_type, g.x_scales != nullptr ? v * g.x_scales[m] : v);
   }
 }
 
 template <awe_dtype T, int kM>
 awe_status launch_rows(const W4Args& a, bool fine, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.g.N + 15) / 16), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM)));
-  if (fine)
-    hipLaunchKernelGGL((w4_rows_kernel<T, kM, true>), grid, dim3(512), 0, stream, a);
+  const dim3 grid((unsigned)((a.g.N + 15) / 16), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM))), block(64 * kW);
+  const bool s4 = a.g.s_type == AWE_F32;
+  if (fine && s4)
+    hipLaunchKernelGGL((w4_rows_kernel<T, kM, true, true>), grid, block, 0, stream, a);
+  else if (fine)
+    hipLaunchKernelGGL((w4_rows_kernel<T, kM, true, false>), grid, block, 0, stream, a);
+  else if (s4)
+    hipLaunchKernelGGL((w4_rows_kernel<T, kM, false, true>), grid, block, 0, stream, a);
   else
-    hipLaunchKernelGGL((w4_rows_kernel<T, kM, false>), grid, dim3(512), 0, stream, a);
+    hipLaunchKernelGGL((w4_rows_kernel<T, kM, false, false>), grid, block, 0, stream, a);
   return launched("w4 launch");
 }
 
@@ -326,8 +373,12 @@ awe_status launch_kind(const W4Args& a, bool fine, hipStream_t stream) {
 awe_status launch_w4(const W4Launch& g, hipStream_t stream) {
   // one group of at least K indices counts as a long one
   const bool fine = g.group % kChunk != 0 && g.group < g.K;
-  const int64_t group = g.group < g.K ? g.group : (g.K + kChunk - 1) / kChunk * kChunk;
-  W4Args a{g, (int32_t)std::max<int64_t>(1, group / (fine ? 32 : kChunk))};
+  W4Args a{g, 1, 0, 0};
+  if (g.group >= g.K) a.g.group = std::max<int64_t>(1, (g.K + kChunk - 1) / kChunk) * kChunk;
+  a.units = (int32_t)(a.g.group / (fine ? 32 : kChunk));
+  const int32_t units = kW * (fine ? 4 : 1);  // of kW chunks
+  a.step_g = units / a.units;
+  a.step_u = units % a.units;
   if (g.x_type == AWE_BF16) return launch_kind<AWE_BF16>(a, fine, stream);
   if (g.x_type == AWE_F16) return launch_kind<AWE_F16>(a, fine, stream);
   return launch_kind<AWE_I8>(a, fine, stream);
