@@ -117,11 +117,6 @@ __device__ __forceinline__ typename Kind<T>::Raw load8(const typename Kind<T>::E
     return u4{a.w[0], a.w[1], a.w[2], a.w[3]};
   }
 }
-template <awe_dtype T>
-__device__ __forceinline__ typename Kind<T>::Raw none() {
-  return typename Kind<T>::Raw{};
-}
-
 // Words of the four quarters of a wave transposed: word j of quarter q becomes word q of quarter j.
 __device__ __forceinline__ u4 across_quarters(u4 w) {
   auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
@@ -135,237 +130,232 @@ constexpr int kChunk = 128;  // reduction indices of a wave's step: 16 bytes of 
 
 struct W4Args {
   W4Launch g;
-  int32_t units;           // group / 128, or group / 32 where 128 does not divide it
-  int32_t step_g, step_u;  // 8 chunks are step_g groups and step_u units
+  int32_t units;      // group / 128, or group / 32 where 128 does not divide it
 };
 
-// The chunk of a lane: row n of W at indices 32 q .. 32 q + 31 of the chunk.  kFine: a group may begin at any
-// multiple of 32 indices, so each product of 32 indices has to lie in one group: the words are
-// transposed over the quarters, and step j covers indices 32 j .. 32 j + 31 (8 q .. 8 q + 7 of them in
-// this lane); otherwise step j covers 8 j .. 8 j + 7 of every quarter's 32.
-template <bool kFine>
-__device__ __forceinline__ int step_offset(int q, int j) {
-  return kFine ? 32 * j + 8 * q : 32 * q + 8 * j;
+// A lane loads row n of W at indices 32 q .. 32 q + 31 of the chunk (16 bytes); the words are then transposed over
+// the quarters, so that step j covers indices 32 j .. 32 j + 31, 8 q .. 8 q + 7 of them in this lane: a step
+// lies in one group (groups begin at multiples of 32 indices), and a load of X's operand reads 64 (int8: 32) adjacent bytes
+// of each row.
+__device__ __forceinline__ int step_offset(int q, int j) { return 32 * j + 8 * q; }
+
+// 16 bytes at byte `at` of a row of `bytes` bytes, 0 past its end (nothing there is read).
+__device__ u4 row_end(const uint8_t* row, int64_t at, int64_t bytes) {
+  u4 r = {0, 0, 0, 0};
+  const int n = (int)std::max<int64_t>(0, std::min<int64_t>(bytes - at, 16));
+#pragma unroll
+  for (int b = 0; b < 16; ++b) r[b >> 2] |= (b < n ? (uint32_t)row[at + b] : 0u) << (8 * (b & 3));
+  return r;
 }
 
 // A scale as it lies in memory, and its value.
-template <bool kS4>
-__device__ __forceinline__ uint32_t raw_scale(const void* p, int64_t i) {
-  if constexpr (kS4)
-    return reinterpret_cast<const uint32_t*>(p)[i];
+template <awe_dtype S>
+__device__ __forceinline__ uint32_t raw_scale(const uint8_t* p) {
+  if constexpr (S == AWE_F32)
+    return *reinterpret_cast<const uint32_t*>(p);
   else
-    return reinterpret_cast<const uint16_t*>(p)[i];
+    return *reinterpret_cast<const uint16_t*>(p);
 }
-template <bool kS4>
-__device__ __forceinline__ float scale_value(uint32_t raw, bool is_bf16) {
-  if constexpr (kS4) return __builtin_bit_cast(float, raw);
-  const float h = (float)__builtin_bit_cast(_Float16, (uint16_t)raw);
-  return is_bf16 ? __builtin_bit_cast(float, raw << 16) : h;
+template <awe_dtype S>
+__device__ __forceinline__ float scale_value(uint32_t raw) {
+  if constexpr (S == AWE_F32) return __builtin_bit_cast(float, raw);
+  if constexpr (S == AWE_BF16) return __builtin_bit_cast(float, raw << 16);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)raw);
 }
 
-// Few rows: 16 outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
-// with kM x 16 rows of X; operands go straight from memory to the matrix unit.  Bound by the
-// weights' bytes: a wave has kD chunks of them in flight, and the rows of one chunk ahead.
+// Few rows: 16 kN outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
+// with up to kM x 16 rows of X.  Operands go straight from memory to the matrix unit, and a wave's loop is one
+// copy of the code for kD chunks, whose loads the compiler spreads over the products: unrolled
+// further to fetch ahead, it spent more time on fetching instructions than it saved (13.2 us instead of
+// 10.6 for one row at 8192 x 8192; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
 constexpr int kW = 8;
-template <awe_dtype T, int kM, bool kFine, bool kS4>
-__global__ __launch_bounds__(64 * kW, kM == 1 ? 4 : 2) void w4_rows_kernel(W4Args a) {
+
+template <awe_dtype T, int kM, int kN, int kD, bool kFine, awe_dtype S>
+__global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   using X = Kind<T>;
-  constexpr int kD = kFine ? 2 : (kM == 1 ? 8 : 4);   // chunks of W in flight
-  constexpr int kX = kFine && kM == 4 ? 1 : 2;          // chunks of X (kD is a multiple)
-  constexpr int kS = kFine ? 4 : 1;
+  using Elem = typename X::Elem;
+  constexpr int kS = kFine ? kD : 1;
+  constexpr int kE = sizeof(Elem), kSE = S == AWE_F32 ? 4 : 2;
   const W4Launch& g = a.g;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * 16 * kM;
-  const int64_t n = n0 + i < g.N ? n0 + i : g.N - 1;
-  const uint8_t* w = g.w + n * g.ldw + 16 * q;
-  const typename X::Elem* x[kM];
-  bool ok[kM];
-#pragma unroll
-  for (int t = 0; t < kM; ++t) {
-    ok[t] = m0 + 16 * t + i < g.M;
-    x[t] = reinterpret_cast<const typename X::Elem*>(g.x) + (ok[t] ? m0 + 16 * t + i : 0) * g.ldx;
-  }
-  const bool is_bf16 = g.s_type == AWE_BF16, has_z = g.zeros != nullptr;
-  const int64_t s0 = n * g.lds, z0 = n * g.ldz;
-  const uint8_t* zp = has_z ? g.zeros : g.w;  // (any byte, where there are none)
-  const uint32_t magic = X::magic();
-  f4 acc[kM];
-#pragma unroll
-  for (int t = 0; t < kM; ++t) acc[t] = f4{0.f, 0.f, 0.f, 0.f};
+  const int64_t n0 = (int64_t)blockIdx.x * 16 * kN, m0 = (int64_t)blockIdx.y * 16 * kM;
 
-  // adds a group's part: part - (bias + z) sum x, times the group's scale
-  auto fold = [&](const typename X::Acc* part, const typename X::Acc* sum, uint32_t rs, uint32_t rz) {
-    const float s = scale_value<kS4>(rs, is_bf16), b = X::kBias + (has_z ? (float)rz : 8.f);
+  // Each operand: the tile's first row (a scalar address) and this lane's 32-bit offset in bytes.  Past
+  // the last row or output, that one again: its result is not stored.
+  const bool has_z = g.zeros != nullptr;
+  const uint8_t* wb = g.w + n0 * g.ldw;
+  const uint8_t* sb = reinterpret_cast<const uint8_t*>(g.scales) + n0 * g.lds * kSE;
+  const uint8_t* zb = has_z ? g.zeros + n0 * g.ldz : g.w;  // (any byte, where there are none)
+  const uint8_t* xb = reinterpret_cast<const uint8_t*>(g.x) + m0 * g.ldx * kE;
+  uint32_t wo[kN], so[kN], zo[kN], xo[kM];
 #pragma unroll
-    for (int t = 0; t < kM; ++t)
+  for (int t = 0; t < kN; ++t) {
+    const uint32_t n = (uint32_t)std::min<int64_t>(16 * t + i, g.N - 1 - n0);
+    wo[t] = n * (uint32_t)g.ldw + 16 * q;
+    so[t] = n * (uint32_t)g.lds * kSE;
+    zo[t] = has_z ? n * (uint32_t)g.ldz : 0;
+  }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) acc[t][r] += s * ((float)part[t][r] - b * (float)sum[t][r]);
-  };
-  auto chunk = [&](u4 cw, const typename X::Raw (&xr)[kM][4], const uint32_t* s, const uint32_t* z) {
-    typename X::Acc part[kM], sum[kM];
-    if (kFine) cw = across_quarters(cw);
+  for (int t = 0; t < kM; ++t) xo[t] = ((uint32_t)std::min<int64_t>(16 * t + i, g.M - 1 - m0) * (uint32_t)g.ldx + 8 * q) * kE;
+  const uint32_t magic = X::magic();
+  f4 acc[kN][kM];
+#pragma unroll
+  for (int t = 0; t < kN; ++t)
+#pragma unroll
+    for (int u = 0; u < kM; ++u) acc[t][u] = f4{0.f, 0.f, 0.f, 0.f};
+
+  // A chunk's products.  s, z: a lane's scale and zero point of output tile t, in quarter `of` + step (kFine) or
+  // in quarter `of`.
+  auto chunk = [&](const u4 (&cw)[kN], const typename X::Raw (&xr)[kM][4], const uint32_t (&s)[kN], const uint32_t (&z)[kN],
+                   int of) {
+    u4 c[kN];
+#pragma unroll
+    for (int t = 0; t < kN; ++t) c[t] = across_quarters(cw[t]);
+    typename X::Acc part[kN][kM], sum[kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const typename X::Op c = X::codes(cw[j], magic);
       const bool first = kFine || j == 0;
+      typename X::Op e[kM];
 #pragma unroll
-      for (int t = 0; t < kM; ++t) {
-        const typename X::Op e = X::elems(xr[t][j]);
-        part[t] = X::mul(e, c, first ? X::zero() : part[t]);
-        sum[t] = X::mul(e, X::ones(), first ? X::zero() : sum[t]);
+      for (int u = 0; u < kM; ++u) {
+        e[u] = X::elems(xr[u][j]);
+        sum[u] = X::mul(e[u], X::ones(), first ? X::zero() : sum[u]);
       }
-      if (kFine || j == 3) fold(part, sum, s[kFine ? j : 0], z[kFine ? j : 0]);
+#pragma unroll
+      for (int t = 0; t < kN; ++t) {
+        const typename X::Op op = X::codes(c[t][j], magic);
+#pragma unroll
+        for (int u = 0; u < kM; ++u) part[t][u] = X::mul(e[u], op, first ? X::zero() : part[t][u]);
+      }
+      if (!kFine && j < 3) continue;
+      // a group's part: part - (bias + z) sum x, times the group's scale
+#pragma unroll
+      for (int t = 0; t < kN; ++t) {
+        const int from = 16 * (kFine ? j : of) + i;
+        const float sc = scale_value<S>(__shfl(s[t], from)), b = X::kBias + (has_z ? (float)__shfl(z[t], from) : 8.f);
+#pragma unroll
+        for (int u = 0; u < kM; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[t][u][r] += sc * ((float)part[t][u][r] - b * (float)sum[u][r]);
+      }
     }
   };
-  // Scales and zero points of the lane's output in the groups of a chunk whose first unit is unit `u` of
-  // group `grp`; groups past `last` are not touched.
-  auto scales = [&](int32_t grp, int32_t u, int32_t last, uint32_t* s, uint32_t* z) {
+  const int32_t full = (int32_t)(g.K / kChunk), last = (int32_t)((g.K - 1) / g.group);
+  // this lane's scales in the group of a unit
+  auto scales = [&](uint32_t unit, uint32_t (&s)[kN], uint32_t (&z)[kN]) {
+    const int32_t grp = std::min((int32_t)(unit / (uint32_t)a.units), last);
 #pragma unroll
-    for (int j = 0; j < kS; ++j) {
-      const int32_t at = grp < last ? grp : last;
-      s[j] = raw_scale<kS4>(g.scales, s0 + at);
-      z[j] = zp[has_z ? z0 + at : 0];
-      if (++u == a.units) u = 0, ++grp;
-    }
-  };
-  auto codes = [&](int32_t c) {
-    const Any16 v = *reinterpret_cast<const Any16*>(w + (int64_t)c * (kChunk / 2));
-    return u4{v.w[0], v.w[1], v.w[2], v.w[3]};
-  };
-  auto rows = [&](int32_t c, typename X::Raw (&xr)[kM][4]) {
-#pragma unroll
-    for (int t = 0; t < kM; ++t) {
-      const typename X::Elem* p = x[t] + (int64_t)c * kChunk;
-      if constexpr (T == AWE_I8 && !kFine) {
-#pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const u4 v = ok[t] ? load8<AWE_BF16>(reinterpret_cast<const uint16_t*>(p + step_offset<kFine>(q, j))) : u4{0, 0, 0, 0};
-          xr[t][j] = (uint64_t)v[0] | (uint64_t)v[1] << 32;
-          xr[t][j + 1] = (uint64_t)v[2] | (uint64_t)v[3] << 32;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) xr[t][j] = ok[t] ? load8<T>(p + step_offset<kFine>(q, j)) : none<T>();
-      }
+    for (int t = 0; t < kN; ++t) {
+      s[t] = raw_scale<S>(sb + (so[t] + (uint32_t)grp * kSE));
+      z[t] = zb[zo[t] + (has_z ? (uint32_t)grp : 0)];
     }
   };
 
-  // chunk wave + 8 t begins in unit `unit` of group `grp` (ahead: of the chunk that is fetched next)
-  const int32_t full = (int32_t)(g.K / kChunk);
-  const uint32_t first_unit = (uint32_t)wave * (kFine ? 4 : 1);
-  int32_t grp = (int32_t)(first_unit / (uint32_t)a.units), unit = (int32_t)(first_unit % (uint32_t)a.units);
-  auto next = [&] {
-    grp += a.step_g;
-    unit += a.step_u;
-    if (unit >= a.units) unit -= a.units, ++grp;
-  };
-  const int32_t last = (int32_t)((g.K - 1) / g.group);
-  if (wave < full) {
-    u4 cw[kD];
-    typename X::Raw xr[kX][kM][4];
-    uint32_t s[kD][kS], z[kD][kS];
+#pragma unroll 1
+  for (int32_t c0 = wave; c0 < full; c0 += kW * kD) {  // chunks c0 + u kW
+    u4 cw[kD][kN];
+    typename X::Raw xr[kD][kM][4];
+    uint32_t s[kS][kN], z[kS][kN];
 #pragma unroll
-    for (int u = 0; u < kD; ++u) {  // (past the end: the last chunk again, unused)
-      const int32_t c = wave + u * kW;
-      cw[u] = codes(c < full ? c : full - 1);
-      scales(grp, unit, last, s[u], z[u]);
-      next();
-    }
-    if (kX == 2) rows(wave, xr[0]);
-    for (int32_t c0 = wave; c0 < full; c0 += kW * kD) {
+    for (int u = 0; u < kD; ++u) {
+      const int64_t c = std::min(c0 + u * kW, full - 1);  // (past the end: the last one again, unused)
 #pragma unroll
-      for (int u = 0; u < kD; ++u) {
-        const int32_t c = c0 + u * kW;
-        if (c >= full) break;
-        if (kX == 2)
-          rows(c + kW < full ? c + kW : full - 1, xr[(u + 1) % kX]);
-        else
-          rows(c, xr[0]);
-        chunk(cw[u], xr[u % kX], s[u], z[u]);
-        const int32_t ahead = c + kW * kD;
-        if (ahead < full) {
-          cw[u] = codes(ahead);
-          scales(grp, unit, last, s[u], z[u]);
-          next();
-        }
+      for (int t = 0; t < kN; ++t) {
+        const Any16 v = *reinterpret_cast<const Any16*>(wb + c * (kChunk / 2) + wo[t]);
+        cw[u][t] = u4{v.w[0], v.w[1], v.w[2], v.w[3]};
       }
     }
-  }
-  // the last, short chunk, filled up with zeros in LDS
-  __shared__ union {
-    float red[kW][16 * kM][17];
-    struct {
-      alignas(16) uint8_t w[16][kChunk / 2];
-      alignas(16) typename X::Elem x[16 * kM][kChunk];
-    } end;
-  } lds;
-  if ((int64_t)full * kChunk < g.K) {
-    const int64_t k0 = (int64_t)full * kChunk;
-    const int left = (int)(g.K - k0);
-    for (int e = threadIdx.x; e < 16 * (kChunk / 2); e += 64 * kW) {
-      const int64_t row = n0 + e / (kChunk / 2);
-      const int b = e % (kChunk / 2);
-      lds.end.w[e / (kChunk / 2)][b] = row < g.N && 2 * b < left ? g.w[row * g.ldw + k0 / 2 + b] : 0;
-    }
-    for (int e = threadIdx.x; e < 16 * kM * kChunk; e += 64 * kW) {
-      const int64_t row = m0 + e / kChunk;
-      const int k = e % kChunk;
-      lds.end.x[e / kChunk][k] =
-          row < g.M && k < left ? reinterpret_cast<const typename X::Elem*>(g.x)[row * g.ldx + k0 + k] : 0;
-    }
-    __syncthreads();
-    if (full % kW == wave) {
-      const u4 cw = *reinterpret_cast<const u4*>(&lds.end.w[i][16 * q]);
-      typename X::Raw xr[kM][4];
+    // quarter q fetches the scales of the q-th chunk (of step q of each, if fine)
+#pragma unroll
+    for (int v = 0; v < kS; ++v) scales(kFine ? 4 * (c0 + v * kW) + q : c0 + q * kW, s[v], z[v]);
+#pragma unroll
+    for (int u = 0; u < kD; ++u) {
+      const int64_t c = std::min(c0 + u * kW, full - 1);
 #pragma unroll
       for (int t = 0; t < kM; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          xr[t][j] = *reinterpret_cast<const typename X::Raw*>(&lds.end.x[16 * t + i][step_offset<kFine>(q, j)]);
-      uint32_t s[kS], z[kS];
-      const uint32_t u0 = (uint32_t)full * (kFine ? 4 : 1);
-      scales((int32_t)(u0 / (uint32_t)a.units), (int32_t)(u0 % (uint32_t)a.units), last, s, z);
-      chunk(cw, xr, s, z);
+        for (int j = 0; j < 4; ++j) xr[u][t][j] = load8<T>(reinterpret_cast<const Elem*>(xb + (c * kChunk + 32 * j) * kE + xo[t]));
+    }
+#pragma unroll
+    for (int u = 0; u < kD; ++u) {
+      if (c0 + u * kW >= full) break;
+      chunk(cw[u], xr[u], s[kFine ? u : 0], z[kFine ? u : 0], u);
+    }
+  }
+
+  // the last, short chunk, X filled up with zeros in LDS
+  __shared__ union {
+    float red[kW][16 * kM][16 * kN + 1];
+    alignas(16) Elem x[16 * kM][kChunk];
+  } lds;
+  if ((int64_t)full * kChunk < g.K) {
+    const int64_t k0 = (int64_t)full * kChunk;
+    for (int e = threadIdx.x; e < 16 * kM * kChunk; e += 64 * kW) {
+      const int64_t row = m0 + e / kChunk, k = k0 + e % kChunk;
+      lds.x[e / kChunk][e % kChunk] = row < g.M && k < g.K ? reinterpret_cast<const Elem*>(g.x)[row * g.ldx + k] : 0;
+    }
+    __syncthreads();
+    if (full % kW == wave) {
+      u4 cw[kN];
+      typename X::Raw xr[kM][4];
+      uint32_t s[kN], z[kN];
+#pragma unroll
+      for (int t = 0; t < kN; ++t) cw[t] = row_end(wb + (wo[t] - 16 * q), k0 / 2 + 16 * q, (g.K + 1) / 2);
+#pragma unroll
+      for (int t = 0; t < kM; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) xr[t][j] = *reinterpret_cast<const typename X::Raw*>(&lds.x[16 * t + i][step_offset(q, j)]);
+      scales(kFine ? 4 * full + q : full, s, z);
+      chunk(cw, xr, s, z, 0);
     }
     __syncthreads();
   }
 
   // the waves' sums, and Y
 #pragma unroll
-  for (int t = 0; t < kM; ++t)
+  for (int t = 0; t < kN; ++t)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) lds.red[wave][16 * t + 4 * q + r][i] = acc[t][r];
+    for (int u = 0; u < kM; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) lds.red[wave][16 * u + 4 * q + r][16 * t + i] = acc[t][u][r];
   __syncthreads();
-  for (int e = threadIdx.x; e < 256 * kM; e += 64 * kW) {
-    const int64_t m = m0 + (e >> 4), j = n0 + (e & 15);
+  for (int e = threadIdx.x; e < 256 * kM * kN; e += 64 * kW) {
+    const int row = e / (16 * kN), col = e % (16 * kN);
+    const int64_t m = m0 + row, j = n0 + col;
     if (m >= g.M || j >= g.N) continue;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < kW; ++k) v += lds.red[k][e >> 4][e & 15];
+    for (int k = 0; k < kW; ++k) v += lds.red[k][row][col];
     store_real(g.y, m * g.ldy + j, g.y_type, g.x_scales != nullptr ? v * g.x_scales[m] : v);
   }
 }
 
-template <awe_dtype T, int kM>
+template <awe_dtype T, int kM, int kN, int kD>
 awe_status launch_rows(const W4Args& a, bool fine, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.g.N + 15) / 16), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM))), block(64 * kW);
-  const bool s4 = a.g.s_type == AWE_F32;
-  if (fine && s4)
-    hipLaunchKernelGGL((w4_rows_kernel<T, kM, true, true>), grid, block, 0, stream, a);
-  else if (fine)
-    hipLaunchKernelGGL((w4_rows_kernel<T, kM, true, false>), grid, block, 0, stream, a);
-  else if (s4)
-    hipLaunchKernelGGL((w4_rows_kernel<T, kM, false, true>), grid, block, 0, stream, a);
+  const dim3 grid((unsigned)((a.g.N + 16 * kN - 1) / (16 * kN)), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM)));
+  const dim3 block(64 * kW);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
+  if (a.g.s_type == AWE_F32)
+    fine ? launch(w4_rows_kernel<T, kM, kN, kD, true, AWE_F32>) : launch(w4_rows_kernel<T, kM, kN, kD, false, AWE_F32>);
+  else if (a.g.s_type == AWE_BF16)
+    fine ? launch(w4_rows_kernel<T, kM, kN, kD, true, AWE_BF16>) : launch(w4_rows_kernel<T, kM, kN, kD, false, AWE_BF16>);
   else
-    hipLaunchKernelGGL((w4_rows_kernel<T, kM, false, false>), grid, block, 0, stream, a);
+    fine ? launch(w4_rows_kernel<T, kM, kN, kD, true, AWE_F16>) : launch(w4_rows_kernel<T, kM, kN, kD, false, AWE_F16>);
   return launched("w4 launch");
 }
 
 template <awe_dtype T>
 awe_status launch_kind(const W4Args& a, bool fine, hipStream_t stream) {
-  if (a.g.M <= 16) return launch_rows<T, 1>(a, fine, stream);
-  if (a.g.M <= 32) return launch_rows<T, 2>(a, fine, stream);
-  return launch_rows<T, 4>(a, fine, stream);
+  if (a.g.M <= 16) {
+    switch (getenv("TRYN") ? atoi(getenv("TRYN")) : 0) {
+      case 1: return launch_rows<T, 1, 1, 4>(a, fine, stream);
+      default: return launch_rows<T, 1, 2, 4>(a, fine, stream);
+    }
+  }
+    switch (getenv("TRYN") ? atoi(getenv("TRYN")) : 0) {
+      case 1: return launch_rows<T, 4, 1, 2>(a, fine, stream);
+      default: return launch_rows<T, 2, 2, 2>(a, fine, stream);
+    }
 }
 
 }  // namespace
@@ -373,12 +363,10 @@ awe_status launch_kind(const W4Args& a, bool fine, hipStream_t stream) {
 awe_status launch_w4(const W4Launch& g, hipStream_t stream) {
   // one group of at least K indices counts as a long one
   const bool fine = g.group % kChunk != 0 && g.group < g.K;
-  W4Args a{g, 1, 0, 0};
+  W4Args a{};
+  a.g = g;
   if (g.group >= g.K) a.g.group = std::max<int64_t>(1, (g.K + kChunk - 1) / kChunk) * kChunk;
   a.units = (int32_t)(a.g.group / (fine ? 32 : kChunk));
-  const int32_t units = kW * (fine ? 4 : 1);  // of kW chunks
-  a.step_g = units / a.units;
-  a.step_u = units % a.units;
   if (g.x_type == AWE_BF16) return launch_kind<AWE_BF16>(a, fine, stream);
   if (g.x_type == AWE_F16) return launch_kind<AWE_F16>(a, fine, stream);
   return launch_kind<AWE_I8>(a, fine, stream);
