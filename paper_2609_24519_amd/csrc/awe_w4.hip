@@ -12,7 +12,9 @@
 namespace awe {
 namespace {
 
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
@@ -50,7 +52,16 @@ struct Kind<AWE_BF16> {
   using Raw = u4;  // eight elements
   using Op = u4;
   using Acc = f4;
+  using Sum = float;
   static constexpr float kBias = 16.f;
+  static __device__ __forceinline__ Sum add(const Op& x, Sum s) {  // the elements' sum
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t pair = x[w];  // (bit_cast of the element itself takes the first one)
+      s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, pair), __builtin_bit_cast(b2, 0x3f803f80u), s, false);
+    }
+    return s;
+  }
   static __device__ __forceinline__ uint32_t magic() { return in_vector(0x41804180u); }  // 16
   static __device__ __forceinline__ Op codes(uint32_t w, uint32_t magic) {
     constexpr uint32_t mask = 0x00780078u;  // a code's place in the mantissa of 16
@@ -70,7 +81,16 @@ struct Kind<AWE_F16> {
   using Raw = u4;
   using Op = u4;
   using Acc = f4;
+  using Sum = float;
   static constexpr float kBias = 16.f;
+  static __device__ __forceinline__ Sum add(const Op& x, Sum s) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t pair = x[w];
+      s = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, pair), __builtin_bit_cast(h2, 0x3c003c00u), s, false);
+    }
+    return s;
+  }
   static __device__ __forceinline__ uint32_t magic() { return in_vector(0x4c004c00u); }
   static __device__ __forceinline__ Op codes(uint32_t w, uint32_t magic) {
     constexpr uint32_t mask = 0x03c003c0u;
@@ -90,7 +110,12 @@ struct Kind<AWE_I8> {
   using Raw = uint64_t;
   using Op = uint64_t;
   using Acc = i4;
-  static constexpr float kBias = 0.f;
+  using Sum = int;
+  static constexpr int kBias = 0;
+  static __device__ __forceinline__ Sum add(Op x, Sum s) {
+    s = __builtin_amdgcn_sdot4((int)x, 0x01010101, s, false);
+    return __builtin_amdgcn_sdot4((int)(x >> 32), 0x01010101, s, false);
+  }
   static __device__ __forceinline__ uint32_t magic() { return 0; }
   static __device__ __forceinline__ Op codes(uint32_t w, uint32_t) {
     return (uint64_t)(w & 0x0f0f0f0fu) | (uint64_t)((w >> 4) & 0x0f0f0f0fu) << 32;
@@ -139,13 +164,38 @@ struct W4Args {
 // of each row.
 __device__ __forceinline__ int step_offset(int q, int j) { return 32 * j + 8 * q; }
 
-// 16 bytes at byte `at` of a row of `bytes` bytes, 0 past its end (nothing there is read).
-__device__ u4 row_end(const uint8_t* row, int64_t at, int64_t bytes) {
-  u4 r = {0, 0, 0, 0};
-  const int n = (int)std::max<int64_t>(0, std::min<int64_t>(bytes - at, 16));
+// 128 bits, the low word first, shifted right by n < 128.
+__device__ __forceinline__ u4 shifted(u4 v, int n) {
+  const uint64_t lo = (uint64_t)v[0] | (uint64_t)v[1] << 32, hi = (uint64_t)v[2] | (uint64_t)v[3] << 32;
+  const uint64_t a = n >= 64 ? hi >> (n - 64) : n > 0 ? lo >> n | hi << (64 - n) : lo, b = n >= 64 ? 0 : hi >> n;
+  return u4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+}
+// 16 bytes at byte `at` of a row of `bytes` bytes, 0 past its end (nothing there is read): the row's last 16
+// bytes, shifted into place.
+__device__ __forceinline__ u4 row_end(const uint8_t* row, int64_t at, int64_t bytes) {
+  if (at >= bytes) return u4{0, 0, 0, 0};
+  if (bytes < 16) {
+    u4 r = {0, 0, 0, 0};
+    for (int b = 0; b < (int)(bytes - at); ++b) {
+      const uint32_t v = (uint32_t)row[at + b] << (8 * (b & 3));
 #pragma unroll
-  for (int b = 0; b < 16; ++b) r[b >> 2] |= (b < n ? (uint32_t)row[at + b] : 0u) << (8 * (b & 3));
-  return r;
+      for (int w = 0; w < 4; ++w) r[w] |= w == b >> 2 ? v : 0u;
+    }
+    return r;
+  }
+  const int64_t from = at + 16 <= bytes ? at : bytes - 16;
+  const Any16 v = *reinterpret_cast<const Any16*>(row + from);
+  return shifted(u4{v.w[0], v.w[1], v.w[2], v.w[3]}, 8 * (int)(at - from));
+}
+// Eight elements of a row of K at k, 0 past its end.
+template <awe_dtype T>
+__device__ __forceinline__ typename Kind<T>::Raw load8_end(const typename Kind<T>::Elem* row, int64_t k, int64_t K) {
+  constexpr int kE = sizeof(typename Kind<T>::Elem);
+  const u4 v = row_end(reinterpret_cast<const uint8_t*>(row), k * kE, K * kE);
+  if constexpr (T == AWE_I8)
+    return (uint64_t)v[0] | (uint64_t)v[1] << 32;
+  else
+    return v;
 }
 
 // A scale as it lies in memory, and its value.
@@ -283,34 +333,28 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
     }
   }
 
-  // the last, short chunk, X filled up with zeros in LDS
-  __shared__ union {
-    float red[kW][16 * kM][16 * kN + 1];
-    alignas(16) Elem x[16 * kM][kChunk];
-  } lds;
-  if ((int64_t)full * kChunk < g.K) {
+  // the last, short chunk
+  if ((int64_t)full * kChunk < g.K && full % kW == wave) {
     const int64_t k0 = (int64_t)full * kChunk;
-    for (int e = threadIdx.x; e < 16 * kM * kChunk; e += 64 * kW) {
-      const int64_t row = m0 + e / kChunk, k = k0 + e % kChunk;
-      lds.x[e / kChunk][e % kChunk] = row < g.M && k < g.K ? reinterpret_cast<const Elem*>(g.x)[row * g.ldx + k] : 0;
-    }
-    __syncthreads();
-    if (full % kW == wave) {
-      u4 cw[kN];
-      typename X::Raw xr[kM][4];
-      uint32_t s[kN], z[kN];
+    u4 cw[kN];
+    typename X::Raw xr[kM][4];
+    uint32_t s[kN], z[kN];
 #pragma unroll
-      for (int t = 0; t < kN; ++t) cw[t] = row_end(wb + (wo[t] - 16 * q), k0 / 2 + 16 * q, (g.K + 1) / 2);
+    for (int t = 0; t < kN; ++t) cw[t] = row_end(wb + (wo[t] - 16 * q), k0 / 2 + 16 * q, (g.K + 1) / 2);
 #pragma unroll
-      for (int t = 0; t < kM; ++t)
+    for (int t = 0; t < kM; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) xr[t][j] = *reinterpret_cast<const typename X::Raw*>(&lds.x[16 * t + i][step_offset(q, j)]);
-      scales(kFine ? 4 * full + q : full, s, z);
-      chunk(cw, xr, s, z, 0);
-    }
-    __syncthreads();
+      for (int j = 0; j < 4; ++j) {
+        const Elem* row = reinterpret_cast<const Elem*>(xb + (xo[t] - 8 * q * kE));
+        xr[t][j] = load8_end<T>(row, k0 + step_offset(q, j), g.K);
+      }
+    scales(kFine ? 4 * full + q : full, s, z);
+    chunk(cw, xr, s, z, 0);
   }
 
+  __shared__ struct {
+    float red[kW][16 * kM][16 * kN + 1];
+  } lds;
   // the waves' sums, and Y
 #pragma unroll
   for (int t = 0; t < kN; ++t)
@@ -330,6 +374,209 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   }
 }
 
+// Many rows: a workgroup has 16 kM rows and 64 kN outputs, 16 kN of them each of its four waves, and goes
+// through the reduction chunk by chunk.  The rows of X lie in LDS, twice (one chunk is multiplied while the
+// next one is fetched and put in the order of the codes), together with what the codes' bias makes of each
+// row, -(bias + 8) sum x over a group, which is where a group's sum starts; scales and zero points lie there
+// too, as floats.  A wave's weights go from memory to its registers, and no other wave unpacks them.
+template <awe_dtype T, int kM, int kN, bool kFine>
+__global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
+  using X = Kind<T>;
+  using Elem = typename X::Elem;
+  using Raw = typename X::Raw;
+  using Acc = typename X::Acc;
+  using Sum = typename X::Sum;
+  constexpr int kE = sizeof(Elem), kRows = 16 * kM, kCols = 64 * kN, kSub = kFine ? 4 : 1;
+  constexpr int kPer = 256 / kRows;           // threads that fetch a row
+  constexpr int kPieces = kChunk / 8 / kPer;  // pieces of 8 elements each of them has
+  static_assert(kPieces % 4 == 0, "a thread's pieces make up steps of 32 indices");
+  static_assert(kCols == 256, "a thread per output fetches its scale");
+  const W4Launch& g = a.g;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
+  // Workgroups go round the eight XCDs; each takes a run of tiles, eight tiles high, so that the ones it
+  // works on at a time share rows and weights in its L2.
+  const int64_t tiles_m = (g.M + kRows - 1) / kRows, tiles_n = (g.N + kCols - 1) / kCols, tiles = tiles_m * tiles_n;
+  const int64_t per_xcd = (tiles + 7) / 8, tile = (int64_t)(blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per_xcd || tile >= tiles) return;
+  const int64_t band = tile / (8 * tiles_n), high = std::min<int64_t>(8, tiles_m - 8 * band), in = tile - band * 8 * tiles_n;
+  const int64_t m0 = (8 * band + in % high) * kRows, n0 = in / high * kCols;
+
+  __shared__ struct {
+    alignas(16) uint8_t x[2][kRows * kChunk * kE];
+    alignas(16) Sum start[2][kSub][kRows], sum[2][kSub][kRows];
+    float s[2][kSub][kCols], z[2][kSub][kCols];
+  } lds;
+  // where a row's piece of 8 elements lies: units of 16 bytes, permuted by the row, so that the same
+  // piece of 16 rows lies in different banks
+  auto place = [](int row, int piece) {
+    return kE == 2 ? row * 256 + ((piece ^ (row & 15)) << 4) : row * 128 + (((piece >> 1) ^ (row & 7)) << 4) + 8 * (piece & 1);
+  };
+
+  // this thread's part of the fetching: pieces first .. first + kPieces - 1 of a row, and the scale of an output
+  const int my_row = threadIdx.x / kPer, first = threadIdx.x % kPer * kPieces;
+  const Elem* xp = reinterpret_cast<const Elem*>(g.x) + std::min<int64_t>(m0 + my_row, g.M - 1) * g.ldx;
+  const int64_t my_col = std::min<int64_t>(n0 + threadIdx.x, g.N - 1);
+  const int32_t full = (int32_t)(g.K / kChunk), chunks = (int32_t)((g.K + kChunk - 1) / kChunk);
+  const int32_t last = (int32_t)((g.K - 1) / g.group);
+  struct Fetched {
+    Raw x[kPieces];
+    float s[kSub], z[kSub];
+  };
+  auto fetch = [&](Fetched& f, int32_t c, bool end) {
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const int64_t k = (int64_t)c * kChunk + 8 * (first + p);
+      f.x[p] = end ? load8_end<T>(xp, k, g.K) : load8<T>(xp + k);
+    }
+#pragma unroll
+    for (int j = 0; j < kSub; ++j) {
+      const int32_t grp = std::min((int32_t)((uint32_t)(kFine ? 4 * c + j : c) / (uint32_t)a.units), last);
+      f.s[j] = load_real(g.scales, my_col * g.lds + grp, g.s_type);
+      f.z[j] = g.zeros != nullptr ? (float)g.zeros[my_col * g.ldz + grp] : 8.f;
+    }
+  };
+  auto keep = [&](const Fetched& f, int buf) {
+    Sum sum[kPieces / 4] = {};
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      const typename X::Op e = X::elems(f.x[p]);
+      sum[p / 4] = X::add(e, sum[p / 4]);
+      *reinterpret_cast<typename X::Op*>(lds.x[buf] + place(my_row, first + p)) = e;
+    }
+    if (kFine) {
+#pragma unroll
+      for (int p = 0; p < kPieces / 4; ++p) {
+        lds.start[buf][first / 4 + p][my_row] = sum[p] * -(X::kBias + 8);
+        lds.sum[buf][first / 4 + p][my_row] = sum[p];
+      }
+    } else {
+#pragma unroll
+      for (int p = 1; p < kPieces / 4; ++p) sum[0] += sum[p];
+#pragma unroll
+      for (int d = 1; d < kPer; d *= 2) sum[0] += __shfl_xor(sum[0], d);
+      if (first == 0) {
+        lds.start[buf][0][my_row] = sum[0] * -(X::kBias + 8);
+        lds.sum[buf][0][my_row] = sum[0];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kSub; ++j) {
+      lds.s[buf][j][threadIdx.x] = f.s[j];
+      lds.z[buf][j][threadIdx.x] = 8.f - f.z[j];  // of sum x, beside what the sum starts from
+    }
+  };
+
+  // this wave's weights
+  const int64_t nw = n0 + 16 * kN * wave;
+  const uint8_t* wb = g.w + std::min(nw, g.N - 1) * g.ldw;
+  uint32_t wo[kN];
+#pragma unroll
+  for (int t = 0; t < kN; ++t)
+    wo[t] = (uint32_t)std::max<int64_t>(0, std::min<int64_t>(16 * t + i, g.N - 1 - nw)) * (uint32_t)g.ldw + 16 * q;
+  auto codes = [&](u4 (&w)[kN], int32_t c, bool end) {
+#pragma unroll
+    for (int t = 0; t < kN; ++t) {
+      if (!end) {
+        const Any16 v = *reinterpret_cast<const Any16*>(wb + (int64_t)c * (kChunk / 2) + wo[t]);
+        w[t] = u4{v.w[0], v.w[1], v.w[2], v.w[3]};
+      } else {
+        w[t] = row_end(wb + (wo[t] - 16 * q), (int64_t)c * (kChunk / 2) + 16 * q, (g.K + 1) / 2);
+      }
+    }
+  };
+
+  const uint32_t magic = X::magic();
+  const bool has_z = g.zeros != nullptr;
+  f4 acc[kN][kM];
+#pragma unroll
+  for (int t = 0; t < kN; ++t)
+#pragma unroll
+    for (int u = 0; u < kM; ++u) acc[t][u] = f4{0.f, 0.f, 0.f, 0.f};
+
+  auto multiply = [&](u4 (&now)[kN], int buf) {
+    Acc part[kN][kM];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int sub = kFine ? j : 0;
+      const bool begin = kFine || j == 0;
+      typename X::Op e[kM];
+      Acc start[kM];
+#pragma unroll
+      for (int u = 0; u < kM; ++u) {
+        e[u] = *reinterpret_cast<const typename X::Op*>(lds.x[buf] + place(16 * u + i, kFine ? 4 * j + q : 4 * q + j));
+        if (begin) start[u] = *reinterpret_cast<const Acc*>(&lds.start[buf][sub][16 * u + 4 * q]);
+      }
+#pragma unroll
+      for (int t = 0; t < kN; ++t) {
+        if (kFine && j == 0) now[t] = across_quarters(now[t]);
+        const typename X::Op op = X::codes(now[t][j], magic);
+#pragma unroll
+        for (int u = 0; u < kM; ++u) part[t][u] = X::mul(e[u], op, begin ? start[u] : part[t][u]);
+      }
+      if (!kFine && j < 3) continue;
+#pragma unroll
+      for (int t = 0; t < kN; ++t) {
+        const int col = 16 * (kN * wave + t) + i;
+        const float sc = lds.s[buf][sub][col];
+#pragma unroll
+        for (int u = 0; u < kM; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[t][u][r] += sc * (float)part[t][u][r];
+        if (has_z) {
+          const float zc = sc * lds.z[buf][sub][col];
+#pragma unroll
+          for (int u = 0; u < kM; ++u) {
+            const Acc st = *reinterpret_cast<const Acc*>(&lds.sum[buf][sub][16 * u + 4 * q]);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[t][u][r] += zc * (float)st[r];
+          }
+        }
+      }
+    }
+  };
+
+  if (full > 0) {
+    Fetched f;
+    u4 now[kN], ahead[kN];
+    codes(now, 0, false);
+    fetch(f, 0, false);
+    keep(f, 0);
+#pragma unroll 1
+    for (int32_t c = 0; c < full; ++c) {
+      __syncthreads();  // chunk c is there, and nobody reads the other half any more
+      if (c + 1 < full) {
+        codes(ahead, c + 1, false);
+        fetch(f, c + 1, false);
+      }
+      multiply(now, c & 1);
+      if (c + 1 < full) keep(f, (c & 1) ^ 1);
+#pragma unroll
+      for (int t = 0; t < kN; ++t) now[t] = ahead[t];
+    }
+  }
+  if (full < chunks) {  // the last, short chunk
+    Fetched f;
+    u4 now[kN];
+    codes(now, full, true);
+    fetch(f, full, true);
+    keep(f, full & 1);
+    __syncthreads();
+    multiply(now, full & 1);
+  }
+
+#pragma unroll
+  for (int u = 0; u < kM; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t m = m0 + 16 * u + 4 * q + r;
+      if (m >= g.M) continue;
+      const float sx = g.x_scales != nullptr ? g.x_scales[m] : 1.f;
+#pragma unroll
+      for (int t = 0; t < kN; ++t)
+        if (nw + 16 * t + i < g.N) store_real(g.y, m * g.ldy + nw + 16 * t + i, g.y_type, acc[t][u][r] * sx);
+    }
+}
+
 template <awe_dtype T, int kM, int kN, int kD>
 awe_status launch_rows(const W4Args& a, bool fine, hipStream_t stream) {
   const dim3 grid((unsigned)((a.g.N + 16 * kN - 1) / (16 * kN)), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM)));
@@ -344,18 +591,26 @@ awe_status launch_rows(const W4Args& a, bool fine, hipStream_t stream) {
   return launched("w4 launch");
 }
 
+template <awe_dtype T, int kM, int kN>
+awe_status launch_tile(const W4Args& a, bool fine, hipStream_t stream) {
+  const int64_t tiles = ((a.g.M + 16 * kM - 1) / (16 * kM)) * ((a.g.N + 64 * kN - 1) / (64 * kN));
+  const int64_t blocks = (tiles + 7) / 8 * 8;
+  if (blocks > 0xffffff) {
+    set_error("too many tiles");
+    return AWE_ERR_UNSUPPORTED;
+  }
+  if (fine)
+    hipLaunchKernelGGL((w4_tile_kernel<T, kM, kN, true>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((w4_tile_kernel<T, kM, kN, false>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  return launched("w4 launch");
+}
+
 template <awe_dtype T>
 awe_status launch_kind(const W4Args& a, bool fine, hipStream_t stream) {
-  if (a.g.M <= 16) {
-    switch (getenv("TRYN") ? atoi(getenv("TRYN")) : 0) {
-      case 1: return launch_rows<T, 1, 1, 4>(a, fine, stream);
-      default: return launch_rows<T, 1, 2, 4>(a, fine, stream);
-    }
-  }
-    switch (getenv("TRYN") ? atoi(getenv("TRYN")) : 0) {
-      case 1: return launch_rows<T, 4, 1, 2>(a, fine, stream);
-      default: return launch_rows<T, 2, 2, 2>(a, fine, stream);
-    }
+  if (a.g.M <= 16) return launch_rows<T, 1, 2, 4>(a, fine, stream);
+  if (a.g.M <= 64) return launch_rows<T, 2, 2, 2>(a, fine, stream);
+  return launch_tile<T, 4, 4>(a, fine, stream);
 }
 
 }  // namespace
