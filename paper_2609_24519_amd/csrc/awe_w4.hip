@@ -379,8 +379,24 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 // next one is fetched and put in the order of the codes), together with what the codes' bias makes of each
 // row, -(bias + 8) sum x over a group, which is where a group's sum starts; scales and zero points lie there
 // too, as floats.  A wave's weights go from memory to its registers, and no other wave unpacks them.
+// kG groups of four waves take the chunks in turn, each with X of its own in LDS, and add up at the end, so that
+// a CU with one workgroup has two waves per SIMD, too.
 template <awe_dtype T, int kM, int kN, bool kFine>
-__global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
+struct TileLds {  // of a group of waves
+  using X = Kind<T>;
+  static constexpr int kRows = 16 * kM, kCols = 64 * kN, kSub = kFine ? 4 : 1;
+  alignas(16) uint8_t x[2][kRows * kChunk * sizeof(typename X::Elem)];
+  alignas(16) typename X::Sum start[2][kSub][kRows], sum[2][kSub][kRows];
+  float s[2][kSub][kCols], z[2][kSub][kCols];
+};
+template <awe_dtype T, int kM, int kN, int kG, bool kFine>
+constexpr int tile_lds_bytes() {
+  const int groups = kG * (int)sizeof(TileLds<T, kM, kN, kFine>), sums = (kG - 1) * 256 * kM * kN * 16;
+  return groups > sums ? groups : sums;
+}
+
+template <awe_dtype T, int kM, int kN, int kG, bool kFine>
+__global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
   using X = Kind<T>;
   using Elem = typename X::Elem;
   using Raw = typename X::Raw;
@@ -390,9 +406,10 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
   constexpr int kPer = 256 / kRows;           // threads that fetch a row
   constexpr int kPieces = kChunk / 8 / kPer;  // pieces of 8 elements each of them has
   static_assert(kPieces % 4 == 0, "a thread's pieces make up steps of 32 indices");
-  static_assert(kCols == 256, "a thread per output fetches its scale");
+  static_assert(kCols <= 256, "a thread per output fetches its scale");
   const W4Launch& g = a.g;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane >> 4, i = lane & 15;
   // Workgroups go round the eight XCDs; each takes a run of tiles, eight tiles high, so that the ones it
   // works on at a time share rows and weights in its L2.
   const int64_t tiles_m = (g.M + kRows - 1) / kRows, tiles_n = (g.N + kCols - 1) / kCols, tiles = tiles_m * tiles_n;
@@ -401,11 +418,8 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
   const int64_t band = tile / (8 * tiles_n), high = std::min<int64_t>(8, tiles_m - 8 * band), in = tile - band * 8 * tiles_n;
   const int64_t m0 = (8 * band + in % high) * kRows, n0 = in / high * kCols;
 
-  __shared__ struct {
-    alignas(16) uint8_t x[2][kRows * kChunk * kE];
-    alignas(16) Sum start[2][kSub][kRows], sum[2][kSub][kRows];
-    float s[2][kSub][kCols], z[2][kSub][kCols];
-  } lds;
+  extern __shared__ uint8_t tile_lds[];
+  TileLds<T, kM, kN, kFine>& lds = reinterpret_cast<TileLds<T, kM, kN, kFine>*>(tile_lds)[group];
   // where a row's piece of 8 elements lies: units of 16 bytes, permuted by the row, so that the same
   // piece of 16 rows lies in different banks
   auto place = [](int row, int piece) {
@@ -413,14 +427,17 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
   };
 
   // this thread's part of the fetching: pieces first .. first + kPieces - 1 of a row, and the scale of an output
-  const int my_row = threadIdx.x / kPer, first = threadIdx.x % kPer * kPieces;
+  const int my_row = tid / kPer, first = tid % kPer * kPieces;
   const Elem* xp = reinterpret_cast<const Elem*>(g.x) + std::min<int64_t>(m0 + my_row, g.M - 1) * g.ldx;
-  const int64_t my_col = std::min<int64_t>(n0 + threadIdx.x, g.N - 1);
+  const int64_t my_col = std::min<int64_t>(n0 + tid, g.N - 1);
   const int32_t full = (int32_t)(g.K / kChunk), chunks = (int32_t)((g.K + kChunk - 1) / kChunk);
   const int32_t last = (int32_t)((g.K - 1) / g.group);
+  const bool has_z = g.zeros != nullptr;
+  const uint8_t* zb = has_z ? g.zeros : g.w;  // (any byte, where there are none)
+  const int s_shift = g.s_type == AWE_F32 ? 2 : 1;
   struct Fetched {
     Raw x[kPieces];
-    float s[kSub], z[kSub];
+    uint32_t s[kSub], z[kSub];  // as they lie in memory: nothing may wait for them here
   };
   auto fetch = [&](Fetched& f, int32_t c, bool end) {
 #pragma unroll
@@ -431,8 +448,9 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
 #pragma unroll
     for (int j = 0; j < kSub; ++j) {
       const int32_t grp = std::min((int32_t)((uint32_t)(kFine ? 4 * c + j : c) / (uint32_t)a.units), last);
-      f.s[j] = load_real(g.scales, my_col * g.lds + grp, g.s_type);
-      f.z[j] = g.zeros != nullptr ? (float)g.zeros[my_col * g.ldz + grp] : 8.f;
+      const uint8_t* s = reinterpret_cast<const uint8_t*>(g.scales) + ((my_col * g.lds + grp) << s_shift);
+      f.s[j] = s_shift == 2 ? raw_scale<AWE_F32>(s) : raw_scale<AWE_F16>(s);
+      f.z[j] = zb[has_z ? my_col * g.ldz + grp : 0];
     }
   };
   auto keep = [&](const Fetched& f, int buf) {
@@ -459,10 +477,13 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
         lds.sum[buf][0][my_row] = sum[0];
       }
     }
+    if (tid >= kCols) return;
 #pragma unroll
     for (int j = 0; j < kSub; ++j) {
-      lds.s[buf][j][threadIdx.x] = f.s[j];
-      lds.z[buf][j][threadIdx.x] = 8.f - f.z[j];  // of sum x, beside what the sum starts from
+      lds.s[buf][j][tid] = g.s_type == AWE_F32    ? scale_value<AWE_F32>(f.s[j])
+                                   : g.s_type == AWE_BF16 ? scale_value<AWE_BF16>(f.s[j])
+                                                          : scale_value<AWE_F16>(f.s[j]);
+      lds.z[buf][j][tid] = has_z ? 8.f - (float)f.z[j] : 0.f;  // of sum x, beside what the sum starts from
     }
   };
 
@@ -486,14 +507,13 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
   };
 
   const uint32_t magic = X::magic();
-  const bool has_z = g.zeros != nullptr;
   f4 acc[kN][kM];
 #pragma unroll
   for (int t = 0; t < kN; ++t)
 #pragma unroll
     for (int u = 0; u < kM; ++u) acc[t][u] = f4{0.f, 0.f, 0.f, 0.f};
 
-  auto multiply = [&](u4 (&now)[kN], int buf) {
+  auto multiply = [&](u4 (&now)[kN], int buf, auto between) {
     Acc part[kN][kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -513,6 +533,7 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
 #pragma unroll
         for (int u = 0; u < kM; ++u) part[t][u] = X::mul(e[u], op, begin ? start[u] : part[t][u]);
       }
+      if (j == 0) between();
       if (!kFine && j < 3) continue;
 #pragma unroll
       for (int t = 0; t < kN; ++t) {
@@ -522,46 +543,78 @@ __global__ __launch_bounds__(256, 1) void w4_tile_kernel(W4Args a) {
         for (int u = 0; u < kM; ++u)
 #pragma unroll
           for (int r = 0; r < 4; ++r) acc[t][u][r] += sc * (float)part[t][u][r];
-        if (has_z) {
-          const float zc = sc * lds.z[buf][sub][col];
+      }
+      if (has_z) {
 #pragma unroll
-          for (int u = 0; u < kM; ++u) {
-            const Acc st = *reinterpret_cast<const Acc*>(&lds.sum[buf][sub][16 * u + 4 * q]);
+        for (int u = 0; u < kM; ++u) start[u] = *reinterpret_cast<const Acc*>(&lds.sum[buf][sub][16 * u + 4 * q]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][u][r] += zc * (float)st[r];
-          }
+        for (int t = 0; t < kN; ++t) {
+          const int col = 16 * (kN * wave + t) + i;
+          const float zc = lds.s[buf][sub][col] * lds.z[buf][sub][col];
+#pragma unroll
+          for (int u = 0; u < kM; ++u)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[t][u][r] += zc * (float)start[u][r];
         }
       }
     }
   };
 
-  if (full > 0) {
+  const int32_t stages = (full + kG - 1) / kG;
+  if (stages > 0) {
     Fetched f;
     u4 now[kN], ahead[kN];
-    codes(now, 0, false);
-    fetch(f, 0, false);
-    keep(f, 0);
+    if (group < full) {
+      codes(now, group, false);
+      fetch(f, group, false);
+      keep(f, 0);
+    }
 #pragma unroll 1
-    for (int32_t c = 0; c < full; ++c) {
+    for (int32_t st = 0; st < stages; ++st) {
+      const int32_t c = kG * st + group;
       __syncthreads();  // chunk c is there, and nobody reads the other half any more
-      if (c + 1 < full) {
-        codes(ahead, c + 1, false);
-        fetch(f, c + 1, false);
+      if (c < full) {
+        multiply(now, st & 1, [&] {
+          if (c + kG < full) {
+            codes(ahead, c + kG, false);
+            fetch(f, c + kG, false);
+          }
+        });
+        if (c + kG < full) keep(f, (st & 1) ^ 1);
       }
-      multiply(now, c & 1);
-      if (c + 1 < full) keep(f, (c & 1) ^ 1);
 #pragma unroll
       for (int t = 0; t < kN; ++t) now[t] = ahead[t];
     }
   }
   if (full < chunks) {  // the last, short chunk
-    Fetched f;
     u4 now[kN];
-    codes(now, full, true);
-    fetch(f, full, true);
-    keep(f, full & 1);
+    if (group == full % kG) {
+      Fetched f;
+      codes(now, full, true);
+      fetch(f, full, true);
+      keep(f, stages & 1);
+    }
     __syncthreads();
-    multiply(now, full & 1);
+    if (group == full % kG) multiply(now, stages & 1, [] {});
+  }
+  if (kG > 1) {
+    float* part = reinterpret_cast<float*>(tile_lds);
+    __syncthreads();
+    if (group == 1)
+#pragma unroll
+      for (int t = 0; t < kN; ++t)
+#pragma unroll
+        for (int u = 0; u < kM; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) part[((t * kM + u) * 4 + r) * 256 + tid] = acc[t][u][r];
+    __syncthreads();
+    if (group == 1) return;
+#pragma unroll
+    for (int t = 0; t < kN; ++t)
+#pragma unroll
+      for (int u = 0; u < kM; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[t][u][r] += part[((t * kM + u) * 4 + r) * 256 + tid];
   }
 
 #pragma unroll
@@ -591,26 +644,38 @@ awe_status launch_rows(const W4Args& a, bool fine, hipStream_t stream) {
   return launched("w4 launch");
 }
 
-template <awe_dtype T, int kM, int kN>
-awe_status launch_tile(const W4Args& a, bool fine, hipStream_t stream) {
-  const int64_t tiles = ((a.g.M + 16 * kM - 1) / (16 * kM)) * ((a.g.N + 64 * kN - 1) / (64 * kN));
-  const int64_t blocks = (tiles + 7) / 8 * 8;
-  if (blocks > 0xffffff) {
+template <awe_dtype T, int kM, int kN, int kG, bool kFine>
+awe_status launch_tile(const W4Args& a, int64_t tiles, hipStream_t stream) {
+  static std::mutex mu;
+  static std::set<int> done;
+  constexpr int bytes = tile_lds_bytes<T, kM, kN, kG, kFine>();
+  static_assert(kG <= 2 && bytes <= 160 * 1024 / (3 - kG), "the workgroups of a CU fit its LDS");
+  auto kernel = w4_tile_kernel<T, kM, kN, kG, kFine>;
+  const awe_status st = set_lds_limit(reinterpret_cast<const void*>(kernel), bytes, mu, done);
+  if (st != AWE_OK) return st;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256 * kG), bytes, stream, a);
+  return launched("w4 launch");
+}
+
+template <awe_dtype T, bool kFine>
+awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
+  auto tiles = [&](int cols) { return ((a.g.M + 63) / 64) * ((a.g.N + cols - 1) / cols); };
+  if (tiles(64) > 0xffffff) {
     set_error("too many tiles");
     return AWE_ERR_UNSUPPORTED;
   }
-  if (fine)
-    hipLaunchKernelGGL((w4_tile_kernel<T, kM, kN, true>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
-  else
-    hipLaunchKernelGGL((w4_tile_kernel<T, kM, kN, false>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
-  return launched("w4 launch");
+  // the widest tile that still gives each of the 256 CUs one; two workgroups per CU where there are enough
+  if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFine>(a, tiles(256), stream);
+  if (tiles(256) >= 256) return launch_tile<T, 4, 4, 2, kFine>(a, tiles(256), stream);
+  if (tiles(128) >= 256) return launch_tile<T, 4, 2, 2, kFine>(a, tiles(128), stream);
+  return launch_tile<T, 4, 1, 2, kFine>(a, tiles(64), stream);
 }
 
 template <awe_dtype T>
 awe_status launch_kind(const W4Args& a, bool fine, hipStream_t stream) {
   if (a.g.M <= 16) return launch_rows<T, 1, 2, 4>(a, fine, stream);
   if (a.g.M <= 64) return launch_rows<T, 2, 2, 2>(a, fine, stream);
-  return launch_tile<T, 4, 4>(a, fine, stream);
+  return fine ? launch_tiles<T, true>(a, stream) : launch_tiles<T, false>(a, stream);
 }
 
 }  // namespace
