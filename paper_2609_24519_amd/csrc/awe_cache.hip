@@ -152,10 +152,27 @@ __device__ __forceinline__ int64_t part_index(const AttendArgs& a, int s, int h,
   return ((((int64_t)s * a.g.c.heads + h) * cols + c) * a.splits + x) * (D + 4);
 }
 
+// A row's element type, and eight elements from any address.
+template <awe_dtype T>
+struct RowType;
+template <>
+struct RowType<AWE_BF16> {
+  using Elem = __bf16;
+};
+template <>
+struct RowType<AWE_F16> {
+  using Elem = _Float16;
+};
+template <class E>
+struct __attribute__((packed)) Any8Of {
+  E v[8];
+};
+
 // kSplit: a workgroup has 16 kQ columns and a chunk of the tokens, which its waves take 64 at a time
 // in turn; otherwise its waves have 16 kQ columns each and all of the tokens.
-template <int D, int kQ, bool kSplit>
+template <awe_dtype T, int D, int kQ, bool kSplit>
 __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
+  using Elem = typename RowType<T>::Elem;
   const awe_cache& c = a.g.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
   const int sid = blockIdx.z, head = blockIdx.y;
@@ -168,6 +185,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   const int32_t from = kSplit ? split * a.chunk : 0;
   if (kSplit && split > 0 && from >= s.len) return;
   int32_t to = kSplit && s.len - from > a.chunk ? from + a.chunk : s.len;
+  if (c.num_blocks == 0 && to > from) {  // every id is out of range
+    to = from;
+    if (a.g.flag != nullptr) *a.g.flag = 1;
+  }
 
   // the columns: how many tokens each sees, and its query
   int32_t last[kQ];
@@ -179,23 +200,23 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     const bool ok = col < cols;
     const int32_t row = ok ? (int32_t)(col / a.share) : 0;
     last[t] = !ok ? 0 : a.g.causal ? s.len - s.rows + row + 1 : s.len;
-    const int64_t at = (int64_t)(s.row0 + row) * a.g.q.row + (int64_t)(head * a.share + (ok ? col % a.share : 0)) * a.g.q.head;
-    float v[D / 32][8];
+    // (past the last column: the first one again, without any token)
+    const Elem* p = reinterpret_cast<const Elem*>(a.g.q.p) + (int64_t)(s.row0 + row) * a.g.q.row +
+                    (int64_t)(head * a.share + (ok ? col % a.share : 0)) * a.g.q.head;
+    Any8Of<Elem> v[D / 32];
     float most = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) v[j] = *reinterpret_cast<const Any8Of<Elem>*>(p + 64 * (j >> 1) + 16 * q4 + 8 * (j & 1));
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int d = 64 * (j >> 1) + 16 * q4 + 8 * (j & 1) + e;
-        v[j][e] = ok ? load_real(a.g.q.p, at + d, a.g.type) : 0.f;
-        most = fmaxf(most, fabsf(v[j][e]));
-      }
+      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)v[j].v[e]));
     most = quarters_max(most);
     const int ex = most > 0.f ? __builtin_amdgcn_frexp_expf(most) : 0;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qf[t][j][e] = (_Float16)ldexpf(v[j][e], 15 - ex);
+      for (int e = 0; e < 8; ++e) qf[t][j][e] = (_Float16)ldexpf((float)v[j].v[e], 15 - ex);
     factor[t] = ldexpf(a.g.scale * kLog2e, ex - 15);
   }
   if (!kSplit && a.g.causal) {
@@ -219,27 +240,45 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   }
 
   const int64_t tile = (int64_t)c.block * D;
-  const int chunk_k = i16 >> 2;
   const int32_t step = kSplit ? kWaves * kTokens : kTokens;
-  for (int32_t t0 = from + (kSplit ? wave * kTokens : 0); t0 < to; t0 += step) {
-    // the blocks of this lane's chunk of keys and chunk of values (-1: past the end, or a bad id)
-    const int32_t pk = t0 + 16 * chunk_k, pv = t0 + 16 * q4;
-    const int32_t ik = pk < s.len ? block_of(c, a.g.b, sid, pk, nullptr) : -1;
-    const int32_t iv = pv < s.len ? block_of(c, a.g.b, sid, pv, a.g.flag) : -1;
-    const int64_t ak = ((int64_t)ik * c.heads + head), av = ((int64_t)iv * c.heads + head);
-    u4 kr[4][D / 64], vr[D / 16];
+  const int32_t* table = a.g.b.blocks + (int64_t)sid * a.g.b.ld_blocks;
+  const int key = 16 * (i16 >> 2);                           // this lane's chunk of keys; of values: 16 q4
+  const int32_t k_lane = (i16 & 3) * D + 16 * q4, v_lane = i16 * c.block;  // and its place in them
+  // The block ids of a step's chunks: as they are in the table, -1 past the sequence's end.
+  auto ids = [&](int32_t t0, int32_t& k, int32_t& v) {
+    k = t0 + key < s.len ? table[(t0 + key) >> a.log2_block] : -1;
+    v = t0 + 16 * q4 < s.len ? table[(t0 + 16 * q4) >> a.log2_block] : -1;
+  };
+  auto valid = [&](int32_t id) { return id >= 0 && id < c.num_blocks; };
+  // (without a valid id block 0 is read, and has no weight)
+  u4 kr[4][D / 64], vr[D / 16];
+  float ks, vs;
+  auto fetch_keys = [&](int32_t t0, int32_t id) {
+    const int8_t* p = c.k + ((int64_t)(valid(id) ? id : 0) * c.heads + head) * tile + ((t0 + key) & (c.block - 1)) * D + k_lane;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int d = 0; d < D / 64; ++d)
-        kr[t][d] = ik < 0 ? u4{0, 0, 0, 0}
-                          : *reinterpret_cast<const u4*>(c.k + ak * tile + ((pk & (c.block - 1)) + 4 * t + (i16 & 3)) * D + 64 * d + 16 * q4);
+      for (int d = 0; d < D / 64; ++d) kr[t][d] = *reinterpret_cast<const u4*>(p + 4 * t * D + 64 * d);
+  };
+  auto fetch_values = [&](int32_t t0, int32_t id) {
+    const int64_t at = (int64_t)(valid(id) ? id : 0) * c.heads + head;
+    const int8_t* p = c.v + at * tile + ((t0 + 16 * q4) & (c.block - 1)) + v_lane;
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d)
-      vr[d] = iv < 0 ? u4{0, 0, 0, 0}
-                     : *reinterpret_cast<const u4*>(c.v + av * tile + (16 * d + i16) * c.block + (pv & (c.block - 1)));
-    const float ks = iv < 0 ? 0.f : c.k_scales[av], vs = iv < 0 ? 0.f : c.v_scales[av];
-
+    for (int d = 0; d < D / 16; ++d) vr[d] = *reinterpret_cast<const u4*>(p + 16 * d * c.block);
+    ks = c.k_scales[at];
+    vs = c.v_scales[at];
+  };
+  int32_t t0 = from + (kSplit ? wave * kTokens : 0);
+  int32_t ik = -1, iv = -1, ik1 = -1, iv1 = -1;
+  if (t0 < to) {
+    ids(t0, ik, iv);
+    fetch_keys(t0, ik);
+    fetch_values(t0, iv);
+    ids(t0 + step, ik1, iv1);
+  }
+  for (; t0 < to; t0 += step) {
+    const bool ok = valid(iv);
+    if (!ok && t0 + 16 * q4 < s.len && a.g.flag != nullptr) *a.g.flag = 1;
     f4 sc[kQ][4];
 #pragma unroll
     for (int t = 0; t < kQ; ++t)
@@ -253,34 +292,37 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int t = 0; t < kQ; ++t) sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][j], sc[t][b], 0, 0, 0);
       }
+    const float ks0 = ok ? ks : 0.f, vs0 = ok ? vs : 0.f;
+    const int32_t pv = t0 + 16 * q4;
+    if (t0 + step < to) fetch_keys(t0 + step, ik1);
 
     // softmax of the lane's 16 tokens of its column, against the running maximum
-    int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
+    int et = vs0 != 0.f ? __builtin_amdgcn_frexp_expf(vs0) : -1000;
     et = max(et, __shfl_xor(et, 16));
     et = max(et, __shfl_xor(et, 32));
     h8 pf[kQ][2];
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
-      const float f = factor[t] * ks;
+      const float f = factor[t] * ks0;
+      const int32_t see = ok ? last[t] - pv : 0;  // of the lane's tokens, the first so many
       float top = -INFINITY;
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool see = iv >= 0 && pv + 4 * b + r < last[t];
-          sc[t][b][r] = see ? sc[t][b][r] * f : -INFINITY;
+          sc[t][b][r] = 4 * b + r < see ? sc[t][b][r] * f : -INFINITY;
           top = fmaxf(top, sc[t][b][r]);
         }
       const float now = fmaxf(m[t], quarters_max(top));
       const float base = now == -INFINITY ? 0.f : now;
       const int e = max(ev[t], et);
-      const float keep = ldexpf(__builtin_amdgcn_exp2f(m[t] - base), ev[t] - e);
-      l[t] *= __builtin_amdgcn_exp2f(m[t] - base);
+      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, ev[t] - e);
+      l[t] *= drop;
       m[t] = now;
       ev[t] = e;
       // a weight times its block's scale, below 2^15 times the largest scale so far: FP16 keeps
       // 11 bits of what is at least 2^-29 of the largest, and to 2^-40 of it of the rest
-      const float w = ldexpf(vs, 15 - e);
+      const float w = ldexpf(vs0, 15 - e);
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -300,6 +342,11 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 #pragma unroll
         for (int t = 0; t < kQ; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][e], o[t][d], 0, 0, 0);
       }
+    if (t0 + step < to) {
+      fetch_values(t0 + step, iv1);
+      iv = iv1;
+      ids(t0 + 2 * step, ik1, iv1);
+    }
   }
 #pragma unroll
   for (int t = 0; t < kQ; ++t) {
@@ -316,12 +363,13 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     for (int t = 0; t < kQ; ++t) {
       const int64_t col = col0 + 16 * t + i16;
       if (col >= cols) continue;
-      const int64_t at = (int64_t)(s.row0 + col / a.share) * a.g.o.row + (head * a.share + col % a.share) * a.g.o.head;
+      Elem* out = reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
+                  (head * a.share + col % a.share) * a.g.o.head;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          store_real(a.g.o.p, at + 16 * d + 4 * q4 + r, a.g.type, l[t] == 0.f ? 0.f : o[t][d][r] / l[t]);
+          out[16 * d + 4 * q4 + r] = (Elem)(l[t] == 0.f ? 0.f : o[t][d][r] / l[t]);
     }
     return;
   }
@@ -354,8 +402,10 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
       }
       if (col >= cols) continue;
       if (whole) {
-        const int64_t at = (int64_t)(s.row0 + col / a.share) * a.g.o.row + (head * a.share + col % a.share) * a.g.o.head;
-        for (int r = 0; r < 4; ++r) store_real(a.g.o.p, at + d0 + d + r, a.g.type, sum == 0.f ? 0.f : v[r] / sum);
+        Elem* out = reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
+                    (head * a.share + col % a.share) * a.g.o.head;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) out[d0 + d + r] = (Elem)(sum == 0.f ? 0.f : v[r] / sum);
       } else {
         float* p = a.part + part_index(a, sid, head, col, split, D);
         *reinterpret_cast<f4*>(p + 4 + d0 + d) = v;
@@ -423,15 +473,15 @@ awe_status launch_cache_load(const CacheLaunch& g, hipStream_t stream) {
 }
 
 namespace {
-template <int D>
-awe_status launch_attend(const AttendArgs& a, int columns, hipStream_t stream) {
+template <awe_dtype T, int D>
+awe_status launch_attend(const AttendArgs& a, bool own_columns, hipStream_t stream) {
   const dim3 block(64 * kWaves);
   const unsigned heads = (unsigned)a.g.c.heads, seqs = (unsigned)a.g.b.sequences;
-  if (columns > 0) {
-    hipLaunchKernelGGL((attend_kernel<D, 2, false>), dim3((unsigned)a.col_groups, heads, seqs), block, 0, stream, a);
+  if (own_columns) {
+    hipLaunchKernelGGL((attend_kernel<T, D, 2, false>), dim3((unsigned)a.col_groups, heads, seqs), block, 0, stream, a);
     return launched("attention launch");
   }
-  hipLaunchKernelGGL((attend_kernel<D, 1, true>), dim3((unsigned)(a.col_groups * a.splits), heads, seqs), block, 0, stream, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, 1, true>), dim3((unsigned)(a.col_groups * a.splits), heads, seqs), block, 0, stream, a);
   awe_status st = launched("attention launch");
   if (st != AWE_OK || a.splits == 1) return st;
   const int64_t cols = a.g.b.max_rows * a.share;
@@ -452,13 +502,19 @@ awe_status launch_cache_attend(const AttendLaunch& g, hipStream_t stream) {
     a.g.b.blocks += s * g.b.ld_blocks;
     if (a.g.b.max_rows > a.g.b.rows) a.g.b.max_rows = a.g.b.rows;
     a.share = g.q_heads / g.c.heads;
+    a.log2_block = __builtin_ctz((unsigned)g.c.block);
     a.chunk = plan.chunk;
     a.splits = plan.splits;
     a.col_groups = plan.groups;
     a.part = reinterpret_cast<float*>(g.ws);
-    const awe_status st = g.c.head_dim == 64    ? launch_attend<64>(a, plan.own_columns, stream)
-                          : g.c.head_dim == 128 ? launch_attend<128>(a, plan.own_columns, stream)
-                                                : launch_attend<256>(a, plan.own_columns, stream);
+    auto launch = [&](auto type) {
+      constexpr awe_dtype T = decltype(type)::value;
+      return g.c.head_dim == 64    ? launch_attend<T, 64>(a, plan.own_columns, stream)
+             : g.c.head_dim == 128 ? launch_attend<T, 128>(a, plan.own_columns, stream)
+                                   : launch_attend<T, 256>(a, plan.own_columns, stream);
+    };
+    const awe_status st = g.type == AWE_BF16 ? launch(std::integral_constant<awe_dtype, AWE_BF16>{})
+                                             : launch(std::integral_constant<awe_dtype, AWE_F16>{});
     if (st != AWE_OK) return st;
   }
   return AWE_OK;
