@@ -171,12 +171,13 @@ struct __attribute__((packed)) Any8Of {
 // kSplit: a workgroup has 16 kQ columns and a chunk of the tokens, which its waves take 64 at a time
 // in turn; otherwise its waves have 16 kQ columns each and all of the tokens.
 template <awe_dtype T, int D, int kQ, bool kSplit>
-__global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
   using Elem = typename RowType<T>::Elem;
   const awe_cache& c = a.g.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
   const int sid = blockIdx.z, head = blockIdx.y;
-  const int group = kSplit ? blockIdx.x / a.splits : blockIdx.x, split = kSplit ? blockIdx.x % a.splits : 0;
+  // (the last columns see the most tokens: they go first)
+  const int group = kSplit ? blockIdx.x / a.splits : a.col_groups - 1 - blockIdx.x, split = kSplit ? blockIdx.x % a.splits : 0;
   const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && blockIdx.x == 0);
   const int64_t cols = (int64_t)s.rows * a.share;
   const int64_t col0 = (kSplit ? group : (int64_t)group * kWaves + wave) * 16 * kQ;
@@ -216,8 +217,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) qf[t][j][e] = (_Float16)ldexpf((float)v[j].v[e], 15 - ex);
-    factor[t] = ldexpf(a.g.scale * kLog2e, ex - 15);
+      for (int e = 0; e < 8; ++e) qf[t][j][e] = (_Float16)ldexpf(a.g.scale < 0.f ? -(float)v[j].v[e] : (float)v[j].v[e], 15 - ex);
+    factor[t] = ldexpf(fabsf(a.g.scale) * kLog2e, ex - 15);
   }
   if (!kSplit && a.g.causal) {
     // the last column's row sees the most tokens
@@ -296,43 +297,64 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
     const int32_t pv = t0 + 16 * q4;
     if (t0 + step < to) fetch_keys(t0 + step, ik1);
 
-    // softmax of the lane's 16 tokens of its column, against the running maximum
+    // Softmax of the lane's 16 tokens of its column, against the running maximum.  They lie in one block, so
+    // the weights times its values' scale, w = vs 2^(15 - e) < 2^15, are exp2 of one linear function of the
+    // scores, and the weights' sum is theirs over w.  FP16 keeps 11 bits of what is at least 2^-29 of the
+    // largest scale so far, and to 2^-40 of it of the rest.
     int et = vs0 != 0.f ? __builtin_amdgcn_frexp_expf(vs0) : -1000;
     et = max(et, __shfl_xor(et, 16));
     et = max(et, __shfl_xor(et, 32));
     h8 pf[kQ][2];
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
-      const float f = factor[t] * ks0;
+      float f = factor[t] * ks0;
       const int32_t see = ok ? last[t] - pv : 0;  // of the lane's tokens, the first so many
-      float top = -INFINITY;
+      if (__any(f == 0.f)) {  // (a masked score times 0 would be no number)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[t][b][r] = f == 0.f ? 0.f : sc[t][b][r];
+        f = f == 0.f ? 1.f : f;
+      }
+      if (__any(see < 16)) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[t][b][r] = 4 * b + r < see ? sc[t][b][r] : -INFINITY;
+      }
+      float top = sc[t][0][0];
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          sc[t][b][r] = 4 * b + r < see ? sc[t][b][r] * f : -INFINITY;
-          top = fmaxf(top, sc[t][b][r]);
-        }
-      const float now = fmaxf(m[t], quarters_max(top));
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[t][b][r]);
+      const float now = fmaxf(m[t], quarters_max(top * f));
       const float base = now == -INFINITY ? 0.f : now;
       const int e = max(ev[t], et);
       const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, ev[t] - e);
-      l[t] *= drop;
       m[t] = now;
       ev[t] = e;
-      // a weight times its block's scale, below 2^15 times the largest scale so far: FP16 keeps
-      // 11 bits of what is at least 2^-29 of the largest, and to 2^-40 of it of the rest
       const float w = ldexpf(vs0, 15 - e);
+      const bool some = !(w < 0x1p-25f);  // (FP16 holds no smaller weight; but it counts in the sum)
+      const float shift = (some ? __builtin_amdgcn_logf(w) : 0.f) - base, per_w = some ? 1.f / w : 1.f;
+      float sum = 0.f;
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(sc[t][b][r] - base);
-          l[t] += p;
-          pf[t][b >> 1][4 * (b & 1) + r] = (_Float16)(p * w);
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][b][r], f, shift));
+          sum += p;
+          pf[t][b >> 1][4 * (b & 1) + r] = (_Float16)p;
         }
+      l[t] = l[t] * drop + sum * per_w;
+      if (__any(!some)) {
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) o[t][d] *= keep;
+        for (int u = 0; u < 2; ++u)
+          if (!some) pf[t][u] = h8{};
+      }
+      if (__any(keep != 1.f)) {
+#pragma unroll
+        for (int d = 0; d < D / 16; ++d) o[t][d] *= keep;
+      }
     }
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
@@ -418,30 +440,59 @@ __global__ __launch_bounds__(64 * kWaves) void attend_kernel(AttendArgs a) {
   }
 }
 
-// Joins the splits of a column: 64 threads per column, D / 64 dimensions each.
-template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a) {
-  const int sid = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63;
+// Joins the splits of a column: a workgroup per column, whose waves take the splits in turn (D / 64
+// dimensions per lane), eight at a time in flight.
+template <awe_dtype T, int D>
+__global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a) {
+  using Elem = typename RowType<T>::Elem;
+  constexpr int kAtOnce = 8;
+  const int sid = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Seq s = sequence(a.g.b, sid, false, nullptr, false);
-  const int64_t col = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t col = blockIdx.x;
   if (s.len <= a.chunk || col >= (int64_t)s.rows * a.share) return;
   const int n = (s.len + a.chunk - 1) / a.chunk;
   const float* p = a.part + part_index(a, sid, head, col, 0, D);
-  float top = -INFINITY, sum = 0.f, v[D / 64] = {};
+  float top = -INFINITY;
   for (int x = lane; x < n; x += 64) top = fmaxf(top, p[(int64_t)x * (D + 4)]);
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll 4
-  for (int x = 0; x < n; ++x) {
-    const float* px = p + (int64_t)x * (D + 4);
-    const float f = __builtin_amdgcn_exp2f(px[0] - base);
-    sum += px[1] * f;
+  float sum = 0.f, v[D / 64] = {};
+  for (int x0 = wave; x0 < n; x0 += kWaves * kAtOnce) {
+    float m[kAtOnce], l[kAtOnce], o[kAtOnce][D / 64];
 #pragma unroll
-    for (int d = 0; d < D / 64; ++d) v[d] += px[4 + 64 * d + lane] * f;
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int x = x0 + u * kWaves;
+      const float* px = p + (int64_t)(x < n ? x : x0) * (D + 4);
+      m[u] = x < n ? px[0] : -INFINITY;
+      l[u] = px[1];
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d) o[u][d] = px[4 + 64 * d + lane];
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (x0 + u * kWaves >= n) break;
+      const float f = __builtin_amdgcn_exp2f(m[u] - base);
+      sum += l[u] * f;
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d) v[d] += o[u][d] * f;
+    }
   }
-  const int64_t at = (int64_t)(s.row0 + col / a.share) * a.g.o.row + (head * a.share + col % a.share) * a.g.o.head;
+  __shared__ float parts[kWaves][D + 1];
 #pragma unroll
-  for (int d = 0; d < D / 64; ++d) store_real(a.g.o.p, at + 64 * d + lane, a.g.type, sum == 0.f ? 0.f : v[d] / sum);
+  for (int d = 0; d < D / 64; ++d) parts[wave][64 * d + lane] = v[d];
+  if (lane == 0) parts[wave][D] = sum;
+  __syncthreads();
+  Elem* out = reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
+              (head * a.share + col % a.share) * a.g.o.head;
+  for (int d = threadIdx.x; d < D; d += 64 * kWaves) {
+    float t = 0.f, w = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+      t += parts[k][D];
+      w += parts[k][d];
+    }
+    out[d] = (Elem)(t == 0.f ? 0.f : w / t);
+  }
 }
 
 // Grid (blocks that can be touched, heads, 2 * sequences); sequences go over in parts of the grid's limit.
@@ -485,7 +536,7 @@ awe_status launch_attend(const AttendArgs& a, bool own_columns, hipStream_t stre
   awe_status st = launched("attention launch");
   if (st != AWE_OK || a.splits == 1) return st;
   const int64_t cols = a.g.b.max_rows * a.share;
-  hipLaunchKernelGGL((attend_join_kernel<D>), dim3((unsigned)((cols + 3) / 4), heads, seqs), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)cols, heads, seqs), block, 0, stream, a);
   return launched("attention join launch");
 }
 }  // namespace

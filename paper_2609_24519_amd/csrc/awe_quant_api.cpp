@@ -156,8 +156,8 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
 }  // namespace
 
 AttendPlan plan_attend(const awe_cache& c, const awe_batch& b, int32_t q_heads) {
-  constexpr int64_t kFill = 2048;   // workgroups that keep the chip busy to the end of ragged sequences
-  constexpr int64_t kChunk = 512;   // fewest tokens worth a workgroup of their own
+  constexpr int64_t kFill = 4096;   // workgroups that keep the chip busy to the end of ragged sequences
+  constexpr int64_t kChunk = 1024;  // fewest tokens worth a workgroup of their own
   const int64_t rows = std::min(b.max_rows, b.rows);
   const int64_t cols = rows * (q_heads / c.heads);
   AttendPlan p{};
