@@ -140,7 +140,7 @@ __device__ __forceinline__ float quarters_max(float x) {
 struct AttendArgs {
   AttendLaunch g;
   int32_t share, log2_block;
-  int32_t chunk;       // tokens of a workgroup (kSplit), a multiple of kWaves * kTokens
+  int32_t chunk;       // tokens of a workgroup that splits them, a multiple of kWaves * kTokens
   int32_t splits;      // workgroups per sequence, head and column tile
   int32_t col_groups;  // column groups (workgroups along the columns) that max_rows asks for
   float* part;         // workspace: kPart(D) floats per column and split
@@ -168,146 +168,65 @@ struct __attribute__((packed)) Any8Of {
   E v[8];
 };
 
-// kSplit: a workgroup has 16 kQ columns and a chunk of the tokens, which its waves take 64 at a time
-// in turn; otherwise its waves have 16 kQ columns each and all of the tokens.
-template <awe_dtype T, int D, int kQ, bool kSplit>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_kernel(AttendArgs a) {
+// What a wave keeps of its 16 kQ columns: queries, running maximum, weights' sum and weighted values.
+template <awe_dtype T, int D, int kQ>
+struct Columns {
   using Elem = typename RowType<T>::Elem;
-  const awe_cache& c = a.g.c;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
-  const int sid = blockIdx.z, head = blockIdx.y;
-  // (the last columns see the most tokens: they go first)
-  const int group = kSplit ? blockIdx.x / a.splits : a.col_groups - 1 - blockIdx.x, split = kSplit ? blockIdx.x % a.splits : 0;
-  const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && blockIdx.x == 0);
-  const int64_t cols = (int64_t)s.rows * a.share;
-  const int64_t col0 = (kSplit ? group : (int64_t)group * kWaves + wave) * 16 * kQ;
-  if (kSplit ? col0 >= cols : (int64_t)group * kWaves * 16 * kQ >= cols) return;
-  // tokens of this workgroup; a sequence without any is one empty chunk
-  const int32_t from = kSplit ? split * a.chunk : 0;
-  if (kSplit && split > 0 && from >= s.len) return;
-  int32_t to = kSplit && s.len - from > a.chunk ? from + a.chunk : s.len;
-  if (c.num_blocks == 0 && to > from) {  // every id is out of range
-    to = from;
-    if (a.g.flag != nullptr) *a.g.flag = 1;
-  }
-
-  // the columns: how many tokens each sees, and its query
-  int32_t last[kQ];
-  float factor[kQ];
-  h8 qf[kQ][D / 32];
-#pragma unroll
-  for (int t = 0; t < kQ; ++t) {
-    const int64_t col = col0 + 16 * t + i16;
-    const bool ok = col < cols;
-    const int32_t row = ok ? (int32_t)(col / a.share) : 0;
-    last[t] = !ok ? 0 : a.g.causal ? s.len - s.rows + row + 1 : s.len;
-    // (past the last column: the first one again, without any token)
-    const Elem* p = reinterpret_cast<const Elem*>(a.g.q.p) + (int64_t)(s.row0 + row) * a.g.q.row +
-                    (int64_t)(head * a.share + (ok ? col % a.share : 0)) * a.g.q.head;
-    Any8Of<Elem> v[D / 32];
-    float most = 0.f;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) v[j] = *reinterpret_cast<const Any8Of<Elem>*>(p + 64 * (j >> 1) + 16 * q4 + 8 * (j & 1));
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)v[j].v[e]));
-    most = quarters_max(most);
-    const int ex = most > 0.f ? __builtin_amdgcn_frexp_expf(most) : 0;
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) qf[t][j][e] = (_Float16)ldexpf(a.g.scale < 0.f ? -(float)v[j].v[e] : (float)v[j].v[e], 15 - ex);
-    factor[t] = ldexpf(fabsf(a.g.scale) * kLog2e, ex - 15);
-  }
-  if (!kSplit && a.g.causal) {
-    // the last column's row sees the most tokens
-    const int64_t end = col0 + 16 * kQ < cols ? col0 + 16 * kQ : cols;
-    const int32_t most = end > col0 ? s.len - s.rows + (int32_t)((end - 1) / a.share) + 1 : 0;
-    to = most < to ? most : to;
-  }
-  if (!kSplit && col0 >= cols) to = 0;
-
+  int64_t col0, cols;  // the first one, and the sequence's
+  int32_t last[kQ];    // tokens that a column sees
+  float factor[kQ];    // of its scores, for powers of two
+  h8 q[kQ][D / 32];
   f4 o[kQ][D / 16];
   float m[kQ], l[kQ];
   int ev[kQ];  // exponent that brings the values' scales seen so far below 1
-#pragma unroll
-  for (int t = 0; t < kQ; ++t) {
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-    ev[t] = -1000;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) o[t][d] = f4{0.f, 0.f, 0.f, 0.f};
-  }
 
-  const int64_t tile = (int64_t)c.block * D;
-  const int32_t step = kSplit ? kWaves * kTokens : kTokens;
-  const int32_t* table = a.g.b.blocks + (int64_t)sid * a.g.b.ld_blocks;
-  const int key = 16 * (i16 >> 2);                           // this lane's chunk of keys; of values: 16 q4
-  const int32_t k_lane = (i16 & 3) * D + 16 * q4, v_lane = i16 * c.block;  // and its place in them
-  // The block ids of a step's chunks: as they are in the table, -1 past the sequence's end.
-  auto ids = [&](int32_t t0, int32_t& k, int32_t& v) {
-    k = t0 + key < s.len ? table[(t0 + key) >> a.log2_block] : -1;
-    v = t0 + 16 * q4 < s.len ? table[(t0 + 16 * q4) >> a.log2_block] : -1;
-  };
-  auto valid = [&](int32_t id) { return id >= 0 && id < c.num_blocks; };
-  // (without a valid id block 0 is read, and has no weight)
-  u4 kr[4][D / 64], vr[D / 16];
-  float ks, vs;
-  auto fetch_keys = [&](int32_t t0, int32_t id) {
-    const int8_t* p = c.k + ((int64_t)(valid(id) ? id : 0) * c.heads + head) * tile + ((t0 + key) & (c.block - 1)) * D + k_lane;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int d = 0; d < D / 64; ++d) kr[t][d] = *reinterpret_cast<const u4*>(p + 4 * t * D + 64 * d);
-  };
-  auto fetch_values = [&](int32_t t0, int32_t id) {
-    const int64_t at = (int64_t)(valid(id) ? id : 0) * c.heads + head;
-    const int8_t* p = c.v + at * tile + ((t0 + 16 * q4) & (c.block - 1)) + v_lane;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) vr[d] = *reinterpret_cast<const u4*>(p + 16 * d * c.block);
-    ks = c.k_scales[at];
-    vs = c.v_scales[at];
-  };
-  int32_t t0 = from + (kSplit ? wave * kTokens : 0);
-  int32_t ik = -1, iv = -1, ik1 = -1, iv1 = -1;
-  if (t0 < to) {
-    ids(t0, ik, iv);
-    fetch_keys(t0, ik);
-    fetch_values(t0, iv);
-    ids(t0 + step, ik1, iv1);
-  }
-  for (; t0 < to; t0 += step) {
-    const bool ok = valid(iv);
-    if (!ok && t0 + 16 * q4 < s.len && a.g.flag != nullptr) *a.g.flag = 1;
-    f4 sc[kQ][4];
-#pragma unroll
-    for (int t = 0; t < kQ; ++t)
-#pragma unroll
-      for (int b = 0; b < 4; ++b) sc[t][b] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        const h8 kf = widen(kr[b][j >> 1][2 * (j & 1)], kr[b][j >> 1][2 * (j & 1) + 1]);
-#pragma unroll
-        for (int t = 0; t < kQ; ++t) sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][j], sc[t][b], 0, 0, 0);
-      }
-    const float ks0 = ok ? ks : 0.f, vs0 = ok ? vs : 0.f;
-    const int32_t pv = t0 + 16 * q4;
-    if (t0 + step < to) fetch_keys(t0 + step, ik1);
-
-    // Softmax of the lane's 16 tokens of its column, against the running maximum.  They lie in one block, so
-    // the weights times its values' scale, w = vs 2^(15 - e) < 2^15, are exp2 of one linear function of the
-    // scores, and the weights' sum is theirs over w.  FP16 keeps 11 bits of what is at least 2^-29 of the
-    // largest scale so far, and to 2^-40 of it of the rest.
-    int et = vs0 != 0.f ? __builtin_amdgcn_frexp_expf(vs0) : -1000;
-    et = max(et, __shfl_xor(et, 16));
-    et = max(et, __shfl_xor(et, 32));
-    h8 pf[kQ][2];
+  __device__ __forceinline__ void begin(const AttendArgs& a, const Seq& s, int head, int64_t first) {
+    const int q4 = (threadIdx.x & 63) >> 4, i16 = threadIdx.x & 15;
+    col0 = first;
+    cols = (int64_t)s.rows * a.share;
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
-      float f = factor[t] * ks0;
+      const int64_t col = col0 + 16 * t + i16;
+      const bool ok = col < cols;
+      const int32_t row = ok ? (int32_t)(col / a.share) : 0;
+      last[t] = !ok ? 0 : a.g.causal ? s.len - s.rows + row + 1 : s.len;
+      // (past the last column: the first one again, without any token)
+      const Elem* p = reinterpret_cast<const Elem*>(a.g.q.p) + (int64_t)(s.row0 + row) * a.g.q.row +
+                      (int64_t)(head * a.share + (ok ? col % a.share : 0)) * a.g.q.head;
+      Any8Of<Elem> v[D / 32];
+      float most = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) v[j] = *reinterpret_cast<const Any8Of<Elem>*>(p + 64 * (j >> 1) + 16 * q4 + 8 * (j & 1));
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf((float)v[j].v[e]));
+      most = quarters_max(most);
+      const int ex = most > 0.f ? __builtin_amdgcn_frexp_expf(most) : 0;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[t][j][e] = (_Float16)ldexpf(a.g.scale < 0.f ? -(float)v[j].v[e] : (float)v[j].v[e], 15 - ex);
+      factor[t] = ldexpf(fabsf(a.g.scale) * kLog2e, ex - 15);
+      m[t] = -INFINITY;
+      l[t] = 0.f;
+      ev[t] = -1000;
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) o[t][d] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // Softmax of the lane's 16 tokens (from token pv on) of its column, against the running maximum: scores to
+  // weights.  They lie in one block, so the weights times its values' scale, w = vs 2^(15 - e) < 2^15, are exp2 of
+  // one linear function of the scores, and the weights' sum is theirs over w.  FP16 keeps 11 bits of what is
+  // at least 2^-29 of the largest scale so far, and to 2^-40 of it of the rest.
+  __device__ __forceinline__ void softmax(f4 (&sc)[kQ][4], h8 (&pf)[kQ][2], bool ok, float ks, float vs, int32_t pv) {
+    int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
+    et = max(et, __shfl_xor(et, 16));
+    et = max(et, __shfl_xor(et, 32));
+#pragma unroll
+    for (int t = 0; t < kQ; ++t) {
+      float f = factor[t] * ks;
       const int32_t see = ok ? last[t] - pv : 0;  // of the lane's tokens, the first so many
       if (__any(f == 0.f)) {  // (a masked score times 0 would be no number)
 #pragma unroll
@@ -333,7 +252,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_kernel(A
       const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, ev[t] - e);
       m[t] = now;
       ev[t] = e;
-      const float w = ldexpf(vs0, 15 - e);
+      const float w = ldexpf(vs, 15 - e);
       const bool some = !(w < 0x1p-25f);  // (FP16 holds no smaller weight; but it counts in the sum)
       const float shift = (some ? __builtin_amdgcn_logf(w) : 0.f) - base, per_w = some ? 1.f / w : 1.f;
       float sum = 0.f;
@@ -356,87 +275,293 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_kernel(A
         for (int d = 0; d < D / 16; ++d) o[t][d] *= keep;
       }
     }
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const h8 vf = widen(vr[d][2 * e], vr[d][2 * e + 1]);
-#pragma unroll
-        for (int t = 0; t < kQ; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][e], o[t][d], 0, 0, 0);
-      }
-    if (t0 + step < to) {
-      fetch_values(t0 + step, iv1);
-      iv = iv1;
-      ids(t0 + 2 * step, ik1, iv1);
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < kQ; ++t) {
-    l[t] += __shfl_xor(l[t], 16);
-    l[t] += __shfl_xor(l[t], 32);
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r], ev[t] - 15);
   }
 
-  if (!kSplit) {
+  // The sums of the quarters, and the values in their own scale.
+  __device__ __forceinline__ void end() {
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
-      const int64_t col = col0 + 16 * t + i16;
-      if (col >= cols) continue;
-      Elem* out = reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
-                  (head * a.share + col % a.share) * a.g.o.head;
+      l[t] += __shfl_xor(l[t], 16);
+      l[t] += __shfl_xor(l[t], 32);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          out[16 * d + 4 * q4 + r] = (Elem)(l[t] == 0.f ? 0.f : o[t][d][r] / l[t]);
+        for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r], ev[t] - 15);
     }
-    return;
   }
+};
+
+// Where a column's result goes.
+template <class Elem>
+__device__ __forceinline__ Elem* result(const AttendArgs& a, const Seq& s, int head, int64_t col) {
+  return reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
+         (head * a.share + col % a.share) * a.g.o.head;
+}
+
+// The cache as a lane sees it, 64 tokens a step: keys' row i of score tile t is token 16 (i / 4) + 4 t + i % 4,
+// values' tokens are 16 q .. 16 q + 15.
+template <int D>
+struct Tokens {
+  const awe_cache& c;
+  const int32_t* table;
+  int64_t tile;
+  int32_t len, head, log2_block, key, value, k_lane, v_lane;
+
+  __device__ __forceinline__ Tokens(const AttendArgs& a, int sid, int head_, int32_t len_)
+      : c(a.g.c), table(a.g.b.blocks + (int64_t)sid * a.g.b.ld_blocks), tile((int64_t)a.g.c.block * D), len(len_), head(head_), log2_block(a.log2_block) {
+    const int q4 = (threadIdx.x & 63) >> 4, i16 = threadIdx.x & 15;
+    key = 16 * (i16 >> 2);
+    value = 16 * q4;
+    k_lane = (i16 & 3) * D + 16 * q4;
+    v_lane = i16 * c.block;
+  }
+  // The block ids of a step's chunks: as they are in the table, -1 past the sequence's end.
+  __device__ __forceinline__ void ids(int32_t t0, int32_t& k, int32_t& v) const {
+    k = t0 + key < len ? table[(t0 + key) >> log2_block] : -1;
+    v = t0 + value < len ? table[(t0 + value) >> log2_block] : -1;
+  }
+  __device__ __forceinline__ bool valid(int32_t id) const { return id >= 0 && id < c.num_blocks; }
+  __device__ __forceinline__ int64_t at(int32_t id) const {  // (without a valid id block 0 is read, and has no weight)
+    return (int64_t)(valid(id) ? id : 0) * c.heads + head;
+  }
+  __device__ __forceinline__ const int8_t* keys(int32_t t0, int32_t id) const {
+    return c.k + at(id) * tile + ((t0 + key) & (c.block - 1)) * D + k_lane;  // + 4 t D + 64 d
+  }
+  __device__ __forceinline__ const int8_t* values(int32_t t0, int32_t id) const {
+    return c.v + at(id) * tile + ((t0 + value) & (c.block - 1)) + v_lane;  // + 16 d block
+  }
+};
+
+// Few columns: a workgroup has 16 of them and a chunk of the tokens, which its waves take 64 at a time in
+// turn.  Bound by the cache's bytes: a wave has a step's keys and values in flight while it works on
+// the step before.
+template <awe_dtype T, int D>
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_split_kernel(AttendArgs a) {
+  using Elem = typename RowType<T>::Elem;
+  const awe_cache& c = a.g.c;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
+  const int sid = blockIdx.z, head = blockIdx.y;
+  const int group = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
+  const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && blockIdx.x == 0);
+  const int64_t cols = (int64_t)s.rows * a.share, col0 = (int64_t)group * 16;
+  if (col0 >= cols) return;
+  // tokens of this workgroup; a sequence without any is one empty chunk
+  const int32_t from = split * a.chunk;
+  if (split > 0 && from >= s.len) return;
+  int32_t to = s.len - from > a.chunk ? from + a.chunk : s.len;
+  if (c.num_blocks == 0 && to > from) {  // every id is out of range
+    to = from;
+    if (a.g.flag != nullptr) *a.g.flag = 1;
+  }
+  Columns<T, D, 1> x;
+  x.begin(a, s, head, col0);
+  const Tokens<D> tokens(a, sid, head, s.len);
+
+  constexpr int32_t step = kWaves * kTokens;
+  u4 kr[4][D / 64], vr[D / 16];
+  float ks = 0.f, vs = 0.f;
+  auto fetch_keys = [&](int32_t t0, int32_t id) {
+    const int8_t* p = tokens.keys(t0, id);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int d = 0; d < D / 64; ++d) kr[t][d] = *reinterpret_cast<const u4*>(p + 4 * t * D + 64 * d);
+  };
+  auto fetch_values = [&](int32_t t0, int32_t id) {
+    const int8_t* p = tokens.values(t0, id);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) vr[d] = *reinterpret_cast<const u4*>(p + 16 * d * c.block);
+    ks = c.k_scales[tokens.at(id)];
+    vs = c.v_scales[tokens.at(id)];
+  };
+  int32_t t0 = from + wave * kTokens;
+  int32_t ik = -1, iv = -1, ik1 = -1, iv1 = -1;
+  if (t0 < to) {
+    tokens.ids(t0, ik, iv);
+    fetch_keys(t0, ik);
+    fetch_values(t0, iv);
+    tokens.ids(t0 + step, ik1, iv1);
+  }
+  for (; t0 < to; t0 += step) {
+    const bool ok = tokens.valid(iv);
+    const int32_t pv = t0 + 16 * q4;
+    if (!ok && pv < s.len && a.g.flag != nullptr) *a.g.flag = 1;
+    f4 sc[1][4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      sc[0][b] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+        sc[0][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(kr[b][j >> 1][2 * (j & 1)], kr[b][j >> 1][2 * (j & 1) + 1]), x.q[0][j], sc[0][b], 0, 0, 0);
+    }
+    const float ks0 = ok ? ks : 0.f, vs0 = ok ? vs : 0.f;
+    if (t0 + step < to) fetch_keys(t0 + step, ik1);
+    h8 pf[1][2];
+    x.softmax(sc, pf, ok, ks0, vs0, pv);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        x.o[0][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(vr[d][2 * e], vr[d][2 * e + 1]), pf[0][e], x.o[0][d], 0, 0, 0);
+    if (t0 + step < to) {
+      fetch_values(t0 + step, iv1);
+      iv = iv1;
+      tokens.ids(t0 + 2 * step, ik1, iv1);
+    }
+  }
+  x.end();
+
   // the waves' parts of each column, through LDS: 64 dimensions at a time
   constexpr int kDim = 64;
   __shared__ float ow[kWaves][16][kDim + 4], mw[kWaves][16], lw[kWaves][16];
   const bool whole = s.len <= a.chunk;
+  const int cl = threadIdx.x >> 4, d = 4 * (threadIdx.x & 15);  // this thread's column and dimensions
+  const int64_t col = col0 + cl;
 #pragma unroll
-  for (int t = 0; t < kQ; ++t) {
+  for (int d0 = 0; d0 < D; d0 += kDim) {
+    __syncthreads();
+    if (q4 == 0 && d0 == 0) {
+      mw[wave][i16] = x.m[0];
+      lw[wave][i16] = x.l[0];
+    }
 #pragma unroll
-    for (int d0 = 0; d0 < D; d0 += kDim) {
-      __syncthreads();
-      if (q4 == 0 && d0 == 0) {
-        mw[wave][i16] = m[t];
-        lw[wave][i16] = l[t];
-      }
+    for (int e = 0; e < kDim / 16; ++e) *reinterpret_cast<f4*>(&ow[wave][i16][16 * e + 4 * q4]) = x.o[0][d0 / 16 + e];
+    __syncthreads();
+    float top = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int d = 0; d < kDim / 16; ++d) *reinterpret_cast<f4*>(&ow[wave][i16][16 * d + 4 * q4]) = o[t][d0 / 16 + d];
-      __syncthreads();
-      // thread: column threadIdx / 16, four dimensions
-      const int cl = threadIdx.x >> 4, d = 4 * (threadIdx.x & 15);
-      const int64_t col = col0 + 16 * t + cl;
-      float top = -INFINITY, sum = 0.f;
-      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mw[w][cl]);
-      f4 v = {0.f, 0.f, 0.f, 0.f};
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(mw[w][cl] - (top == -INFINITY ? 0.f : top));
-        sum += lw[w][cl] * f;
-        v += *reinterpret_cast<const f4*>(&ow[w][cl][d]) * f;
-      }
-      if (col >= cols) continue;
-      if (whole) {
-        Elem* out = reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
-                    (head * a.share + col % a.share) * a.g.o.head;
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mw[w][cl]);
+    f4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) out[d0 + d + r] = (Elem)(sum == 0.f ? 0.f : v[r] / sum);
-      } else {
-        float* p = a.part + part_index(a, sid, head, col, split, D);
-        *reinterpret_cast<f4*>(p + 4 + d0 + d) = v;
-        if (d0 == 0 && d == 0) {
-          p[0] = top;
-          p[1] = sum;
-        }
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(mw[w][cl] - (top == -INFINITY ? 0.f : top));
+      sum += lw[w][cl] * f;
+      v += *reinterpret_cast<const f4*>(&ow[w][cl][d]) * f;
+    }
+    if (col >= cols) continue;
+    if (whole) {
+      Elem* out = result<Elem>(a, s, head, col) + d0 + d;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out[r] = (Elem)(sum == 0.f ? 0.f : v[r] / sum);
+    } else {
+      float* p = a.part + part_index(a, sid, head, col, split, D);
+      *reinterpret_cast<f4*>(p + 4 + d0 + d) = v;
+      if (d0 == 0 && d == 0) {
+        p[0] = top;
+        p[1] = sum;
       }
     }
+  }
+}
+
+// Many columns: each of the kW waves has 16 kQ columns, and together they go through the tokens, 64 a step.
+// A step's keys and values become FP16 once per workgroup: a wave fetches its share as it would for itself, and puts the
+// operands into LDS lane by lane, where every wave reads them as they are (twice: a step's while the
+// next one's are on their way).  Bound by vector instructions, softmax's most of all.
+template <awe_dtype T, int D, int kQ, int kW>
+__global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
+  using Elem = typename RowType<T>::Elem;
+  constexpr int kKeys = 4 * D / 32, kValues = D / 16 * 2;  // operands of a step
+  constexpr int kLoads = D / 16;                            // 16-byte loads of a lane: of keys, and of values
+  const awe_cache& c = a.g.c;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
+  const int sid = blockIdx.z, head = blockIdx.y;
+  const int group = a.col_groups - 1 - blockIdx.x;  // (the last columns see the most tokens: they go first)
+  const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && blockIdx.x == 0);
+  const int64_t cols = (int64_t)s.rows * a.share, first = (int64_t)group * kW * 16 * kQ;
+  if (first >= cols) return;
+  int32_t to = s.len;
+  if (a.g.causal) {  // the last column's row sees the most tokens
+    const int64_t end = std::min<int64_t>(first + kW * 16 * kQ, cols);
+    to = std::min(to, s.len - s.rows + (int32_t)((end - 1) / a.share) + 1);
+  }
+  if (c.num_blocks == 0 && to > 0) {  // every id is out of range
+    to = 0;
+    if (a.g.flag != nullptr) *a.g.flag = 1;
+  }
+  Columns<T, D, kQ> x;
+  x.begin(a, s, head, first + wave * 16 * kQ);
+  const Tokens<D> tokens(a, sid, head, s.len);
+
+  extern __shared__ uint8_t attend_lds[];
+  h8(*lds)[kKeys + kValues][64] = reinterpret_cast<h8(*)[kKeys + kValues][64]>(attend_lds);
+  // this wave's share of a step: loads wave, wave + kW, ... of the 2 kLoads
+  constexpr int kMine = 2 * kLoads / kW;
+  static_assert(kMine * kW == 2 * kLoads, "the waves share the loads evenly");
+  u4 raw[kMine];
+  float ks = 0.f, vs = 0.f;
+  auto fetch = [&](int32_t t0, int32_t ik, int32_t iv) {
+    const int8_t* pk = tokens.keys(t0, ik);
+    const int8_t* pv = tokens.values(t0, iv);
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+      const int load = wave + n * kW;
+      const int8_t* p = load < kLoads ? pk + 4 * (load / (D / 64)) * D + 64 * (load % (D / 64)) : pv + 16 * (load - kLoads) * c.block;
+      raw[n] = *reinterpret_cast<const u4*>(p);
+    }
+    ks = c.k_scales[tokens.at(iv)];
+    vs = c.v_scales[tokens.at(iv)];
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+      const int load = wave + n * kW;
+      lds[buf][2 * load][lane] = widen(raw[n][0], raw[n][1]);
+      lds[buf][2 * load + 1][lane] = widen(raw[n][2], raw[n][3]);
+    }
+  };
+  int32_t ik = -1, iv = -1, ik1 = -1, iv1 = -1;
+  if (to > 0) {
+    tokens.ids(0, ik, iv);
+    fetch(0, ik, iv);
+    tokens.ids(kTokens, ik1, iv1);
+    put(0);
+  }
+  int buf = 0;
+  for (int32_t t0 = 0; t0 < to; t0 += kTokens, buf ^= 1) {
+    __syncthreads();  // the step's operands are there, and nobody reads the other half any more
+    const bool ok = tokens.valid(iv), more = t0 + kTokens < to;
+    const int32_t pv = t0 + 16 * q4;
+    if (!ok && pv < s.len && a.g.flag != nullptr) *a.g.flag = 1;
+    const float ks0 = ok ? ks : 0.f, vs0 = ok ? vs : 0.f;
+    if (more) {
+      fetch(t0 + kTokens, ik1, iv1);
+      iv = iv1;
+      tokens.ids(t0 + 2 * kTokens, ik1, iv1);
+    }
+    f4 sc[kQ][4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+#pragma unroll
+      for (int t = 0; t < kQ; ++t) sc[t][b] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const h8 kf = lds[buf][b * (D / 32) + j][lane];
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, x.q[t][j], sc[t][b], 0, 0, 0);
+      }
+    }
+    h8 pf[kQ][2];
+    x.softmax(sc, pf, ok, ks0, vs0, pv);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const h8 vf = lds[buf][kKeys + 2 * d + e][lane];
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) x.o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][e], x.o[t][d], 0, 0, 0);
+      }
+    if (more) put(buf ^ 1);
+  }
+  x.end();
+#pragma unroll
+  for (int t = 0; t < kQ; ++t) {
+    const int64_t col = x.col0 + 16 * t + i16;
+    if (col >= cols) continue;
+    Elem* out = result<Elem>(a, s, head, col);
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) out[16 * d + 4 * q4 + r] = (Elem)(x.l[t] == 0.f ? 0.f : x.o[t][d][r] / x.l[t]);
   }
 }
 
@@ -526,13 +651,19 @@ awe_status launch_cache_load(const CacheLaunch& g, hipStream_t stream) {
 namespace {
 template <awe_dtype T, int D>
 awe_status launch_attend(const AttendArgs& a, bool own_columns, hipStream_t stream) {
-  const dim3 block(64 * kWaves);
   const unsigned heads = (unsigned)a.g.c.heads, seqs = (unsigned)a.g.b.sequences;
   if (own_columns) {
-    hipLaunchKernelGGL((attend_kernel<T, D, 2, false>), dim3((unsigned)a.col_groups, heads, seqs), block, 0, stream, a);
+    constexpr int kQ = D == 256 ? 1 : 2, kW = kRowsColumns / (16 * kQ), bytes = 2 * (4 * D / 32 + D / 16 * 2) * 1024;
+    static std::mutex mu;
+    static std::set<int> done;
+    auto kernel = attend_rows_kernel<T, D, kQ, kW>;
+    const awe_status st = set_lds_limit(reinterpret_cast<const void*>(kernel), bytes, mu, done);
+    if (st != AWE_OK) return st;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.col_groups, heads, seqs), dim3(64 * kW), bytes, stream, a);
     return launched("attention launch");
   }
-  hipLaunchKernelGGL((attend_kernel<T, D, 1, true>), dim3((unsigned)(a.col_groups * a.splits), heads, seqs), block, 0, stream, a);
+  const dim3 block(64 * kWaves);
+  hipLaunchKernelGGL((attend_split_kernel<T, D>), dim3((unsigned)(a.col_groups * a.splits), heads, seqs), block, 0, stream, a);
   awe_status st = launched("attention launch");
   if (st != AWE_OK || a.splits == 1) return st;
   const int64_t cols = a.g.b.max_rows * a.share;

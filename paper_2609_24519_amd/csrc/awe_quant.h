@@ -55,6 +55,7 @@ struct AttendLaunch {
 };
 awe_status launch_cache_attend(const AttendLaunch& g, hipStream_t stream);
 // How a call is laid over workgroups, from its host-side sizes alone.
+constexpr int kRowsColumns = 128;  // columns of a workgroup whose waves have columns of their own
 struct AttendPlan {
   bool own_columns;  // a wave has columns of its own and sees all tokens; otherwise a workgroup's waves share
                      // 16 columns and split the tokens

@@ -164,7 +164,7 @@ AttendPlan plan_attend(const awe_cache& c, const awe_batch& b, int32_t q_heads) 
   p.own_columns = cols > 32;
   p.splits = 1;
   if (p.own_columns) {
-    p.groups = (int32_t)((cols + 127) / 128);
+    p.groups = (int32_t)((cols + kRowsColumns - 1) / kRowsColumns);
     return p;
   }
   p.groups = (int32_t)((cols + 15) / 16);
