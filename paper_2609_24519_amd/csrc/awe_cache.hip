@@ -178,11 +178,12 @@ struct Columns {
   h8 q[kQ][D / 32];
   f4 o[kQ][D / 16];
   float m[kQ], l[kQ];
-  int ev[kQ];  // exponent that brings the values' scales seen so far below 1
+  int ev;  // exponent that brings the values' scales seen so far below 1
 
   __device__ __forceinline__ void begin(const AttendArgs& a, const Seq& s, int head, int64_t first) {
     const int q4 = (threadIdx.x & 63) >> 4, i16 = threadIdx.x & 15;
     col0 = first;
+    ev = -1000;
     cols = (int64_t)s.rows * a.share;
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
@@ -210,7 +211,6 @@ struct Columns {
       factor[t] = ldexpf(fabsf(a.g.scale) * kLog2e, ex - 15);
       m[t] = -INFINITY;
       l[t] = 0.f;
-      ev[t] = -1000;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[t][d] = f4{0.f, 0.f, 0.f, 0.f};
     }
@@ -224,6 +224,11 @@ struct Columns {
     int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
     et = max(et, __shfl_xor(et, 16));
     et = max(et, __shfl_xor(et, 32));
+    const int e = max(ev, et), rise = ev - e;
+    ev = e;
+    const float w = ldexpf(vs, 15 - e);
+    const bool some = !(w < 0x1p-25f);  // (FP16 holds no smaller weight; but it counts in the sum)
+    const float log_w = some ? __builtin_amdgcn_logf(w) : 0.f, per_w = some ? __builtin_amdgcn_rcpf(w) : 1.f;
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
       float f = factor[t] * ks;
@@ -248,13 +253,8 @@ struct Columns {
         for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[t][b][r]);
       const float now = fmaxf(m[t], quarters_max(top * f));
       const float base = now == -INFINITY ? 0.f : now;
-      const int e = max(ev[t], et);
-      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, ev[t] - e);
+      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, rise), shift = log_w - base;
       m[t] = now;
-      ev[t] = e;
-      const float w = ldexpf(vs, 15 - e);
-      const bool some = !(w < 0x1p-25f);  // (FP16 holds no smaller weight; but it counts in the sum)
-      const float shift = (some ? __builtin_amdgcn_logf(w) : 0.f) - base, per_w = some ? 1.f / w : 1.f;
       float sum = 0.f;
 #pragma unroll
       for (int b = 0; b < 4; ++b)
@@ -286,7 +286,7 @@ struct Columns {
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r], ev[t] - 15);
+        for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r], ev - 15);
     }
   }
 };
@@ -453,6 +453,19 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_split_ke
   }
 }
 
+// Asks for the order of a block of n reads from LDS with kQ products each: six reads ahead of the products.
+template <int n, int kQ>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int kAhead = 6, kMfma = 0x8, kRead = 0x100;
+  __builtin_amdgcn_sched_group_barrier(kRead, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < n - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, kQ, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kMfma, kAhead * kQ, 0);
+}
+
 // Many columns: each of the kW waves has 16 kQ columns, and together they go through the tokens, 64 a step.
 // A step's keys and values become FP16 once per workgroup: a wave fetches its share as it would for itself, and puts the
 // operands into LDS lane by lane, where every wave reads them as they are (twice: a step's while the
@@ -464,9 +477,12 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
   constexpr int kLoads = D / 16;                            // 16-byte loads of a lane: of keys, and of values
   const awe_cache& c = a.g.c;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
-  const int sid = blockIdx.z, head = blockIdx.y;
-  const int group = a.col_groups - 1 - blockIdx.x;  // (the last columns see the most tokens: they go first)
-  const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && blockIdx.x == 0);
+  // The last columns see the most tokens: they go first.  Heads are next to each other, so that with
+  // eight of them the workgroups of a head, which read the same tokens, are on one XCD (293 us instead of
+  // 316 for prompts of up to 2048 tokens; all sequences' last columns first took 491).
+  const uint32_t per_seq = (uint32_t)a.col_groups * a.g.c.heads, in = blockIdx.x % per_seq;
+  const int head = in % a.g.c.heads, sid = blockIdx.x / per_seq, group = a.col_groups - 1 - (int)(in / a.g.c.heads);
+  const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && group == 0);
   const int64_t cols = (int64_t)s.rows * a.share, first = (int64_t)group * kW * 16 * kQ;
   if (first >= cols) return;
   int32_t to = s.len;
@@ -540,6 +556,7 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
         for (int t = 0; t < kQ; ++t) sc[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, x.q[t][j], sc[t][b], 0, 0, 0);
       }
     }
+    reads_ahead<kKeys, kQ>();
     h8 pf[kQ][2];
     x.softmax(sc, pf, ok, ks0, vs0, pv);
 #pragma unroll
@@ -550,6 +567,7 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
 #pragma unroll
         for (int t = 0; t < kQ; ++t) x.o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][e], x.o[t][d], 0, 0, 0);
       }
+    reads_ahead<kValues, kQ>();
     if (more) put(buf ^ 1);
   }
   x.end();
@@ -659,7 +677,7 @@ awe_status launch_attend(const AttendArgs& a, bool own_columns, hipStream_t stre
     auto kernel = attend_rows_kernel<T, D, kQ, kW>;
     const awe_status st = set_lds_limit(reinterpret_cast<const void*>(kernel), bytes, mu, done);
     if (st != AWE_OK) return st;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)a.col_groups, heads, seqs), dim3(64 * kW), bytes, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)a.col_groups * heads * seqs), dim3(64 * kW), bytes, stream, a);
     return launched("attention launch");
   }
   const dim3 block(64 * kWaves);
@@ -675,10 +693,19 @@ awe_status launch_attend(const AttendArgs& a, bool own_columns, hipStream_t stre
 awe_status launch_cache_attend(const AttendLaunch& g, hipStream_t stream) {
   const AttendPlan plan = plan_attend(g.c, g.b, g.q_heads);
   // sequences go over in parts of the grid's limit
-  for (int32_t s = 0; s < g.b.sequences; s += 65535) {
+  int32_t most = 65535;
+  if (plan.own_columns) {
+    const int64_t each = (int64_t)plan.groups * g.c.heads;
+    if (each > 0x7fffff) {
+      set_error("too many rows and heads");
+      return AWE_ERR_UNSUPPORTED;
+    }
+    most = (int32_t)(0x7fffff / each);
+  }
+  for (int32_t s = 0; s < g.b.sequences; s += most) {
     AttendArgs a{};
     a.g = g;
-    a.g.b.sequences = g.b.sequences - s < 65535 ? g.b.sequences - s : 65535;
+    a.g.b.sequences = std::min(most, g.b.sequences - s);
     a.g.b.starts += s;
     a.g.b.lengths += s;
     a.g.b.blocks += s * g.b.ld_blocks;
