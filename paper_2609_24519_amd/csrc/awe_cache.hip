@@ -5,88 +5,158 @@
 namespace awe {
 namespace {
 
-// Where dimension d of slot t lies within its block and head: keys by token, values by dimension.
-__device__ __forceinline__ int64_t element(const awe_cache& c, bool values, int t, int d) {
-  return values ? (int64_t)d * c.block + t : (int64_t)t * c.head_dim + d;
-}
-
+// ---- store and load -------------------------------------------------------------------------
 // One workgroup per touched block, head and tensor: workgroup (j, head, tensor + 2 * sequence) takes the
-// sequence's j-th block that gets rows.
+// sequence's j-th block that gets rows.  Bound by the rows' and the cache's bytes: rows are moved
+// eight elements a thread; values, which are kept by dimension, are turned over in LDS.
 struct Tile {
-  Seq s;
-  int32_t id, first, t0, t1;  // block, position of its slot 0, slots that get rows
+  int32_t id, t0, t1;  // block (-1: nothing to do), slots that get rows
+  int64_t row0;        // row of slot 0 (of slot t0 at the earliest)
 };
-__device__ __forceinline__ Tile tile_of(const CacheLaunch& g, int32_t* flag) {
-  Tile t;
-  t.s = sequence(g.b, blockIdx.z >> 1, true, flag, threadIdx.x == 0);
-  t.id = -1;
-  const int32_t pos0 = t.s.len - t.s.rows;
-  t.first = (pos0 / g.c.block + (int32_t)blockIdx.x) * g.c.block;
-  if (t.s.rows == 0 || t.first >= t.s.len) return t;
-  t.t0 = pos0 > t.first ? pos0 - t.first : 0;
-  t.t1 = t.s.len - t.first < g.c.block ? t.s.len - t.first : g.c.block;
-  t.id = block_of(g.c, g.b, blockIdx.z >> 1, t.first, threadIdx.x == 0 ? flag : nullptr);
-  return t;
+__device__ __forceinline__ Tile tile_of(const CacheLaunch& g) {
+  const bool one = threadIdx.x == 0;
+  const Seq s = sequence(g.b, blockIdx.z >> 1, true, g.flag, one && blockIdx.x == 0);
+  const int32_t pos0 = s.len - s.rows, first = (pos0 / g.c.block + (int32_t)blockIdx.x) * g.c.block;
+  if (s.rows == 0 || first >= s.len) return Tile{-1, 0, 0, 0};
+  const int32_t id = block_of(g.c, g.b, blockIdx.z >> 1, first, one ? g.flag : nullptr);
+  return Tile{id, pos0 > first ? pos0 - first : 0, std::min(s.len - first, g.c.block), (int64_t)s.row0 + first - pos0};
 }
 
-__global__ __launch_bounds__(256) void store_plain_kernel(CacheLaunch g) {
-  const Tile t = tile_of(g, g.flag);
+// Eight elements of a row from any address, as floats.
+template <class E>
+struct __attribute__((packed)) Any8Of {
+  E v[8];
+};
+constexpr float kLargest = 3.402823466e38f;
+
+__device__ __forceinline__ int8_t quantised(float x, float scale) {
+  return scale > 0.f && fabsf(x) <= kLargest ? (int8_t)fminf(fmaxf(rintf(x / scale), -127.f), 127.f) : (int8_t)0;
+}
+
+// Dynamic LDS: a block of values by dimension, rows padded by a word.
+extern __shared__ uint8_t turned[];
+size_t turned_bytes(const awe_cache& c) { return (size_t)c.head_dim * (c.block + 4); }
+
+template <class E>
+__global__ __launch_bounds__(256) void store_kernel(CacheLaunch g) {
+  const Tile t = tile_of(g);
   if (t.id < 0) return;
   const bool values = blockIdx.z & 1;
-  const int head = blockIdx.y, D = g.c.head_dim;
+  const int head = blockIdx.y, D = g.c.head_dim, block = g.c.block, per_row = D / 8;
   const Rows& r = values ? g.v : g.k;
   const int64_t at = (int64_t)t.id * g.c.heads + head;
-  int8_t* q = (values ? g.c.v : g.c.k) + at * g.c.block * D;
+  int8_t* q = (values ? g.c.v : g.c.k) + at * block * D;
   float* scale = (values ? g.c.v_scales : g.c.k_scales) + at;
-  const int64_t row0 = t.s.row0 + (t.first - (t.s.len - t.s.rows));  // row of slot 0
+  const E* rows = reinterpret_cast<const E*>(r.p) + t.row0 * r.row + head * r.head;
+  auto piece = [&](int e) {  // the e-th eight elements
+    return *reinterpret_cast<const Any8Of<E>*>(rows + (t.t0 + e / per_row) * r.row + 8 * (e % per_row));
+  };
+  const int pieces = (t.t1 - t.t0) * per_row;
   float most = 0.f;
   bool bad = false;
-  for (int e = threadIdx.x; e < (t.t1 - t.t0) * D; e += 256) {
-    const float x = fabsf(load_real(r.p, (row0 + t.t0 + e / D) * r.row + head * r.head + e % D, g.type));
-    if (x <= 3.402823466e38f)
-      most = fmaxf(most, x);
-    else
-      bad = true;
-  }
-  if (bad && g.flag != nullptr) *g.flag = 1;
-  __shared__ float part[256];
-  part[threadIdx.x] = most;
-  __syncthreads();
-  for (int d = 128; d > 0; d >>= 1) {
-    if (threadIdx.x < d) part[threadIdx.x] = fmaxf(part[threadIdx.x], part[threadIdx.x + d]);
-    __syncthreads();
-  }
-  const float old = t.t0 > 0 ? *scale : 0.f;
-  const float now = fmaxf(old, part[0] / 127.f);
-  __syncthreads();  // every thread has read the old scale
-  if (threadIdx.x == 0) *scale = now;
-  if (now != old) {
-    const float ratio = old / now;
-    for (int e = threadIdx.x; e < t.t0 * D; e += 256) {
-      int8_t* p = q + element(g.c, values, e / D, e % D);
-      *p = (int8_t)fminf(fmaxf(rintf((float)*p * ratio), -127.f), 127.f);
+  for (int e = threadIdx.x; e < pieces; e += 256) {
+    const Any8Of<E> v = piece(e);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = fabsf((float)v.v[i]);
+      bad |= !(x <= kLargest);
+      most = x <= kLargest ? fmaxf(most, x) : most;
     }
   }
-  for (int e = threadIdx.x; e < (t.t1 - t.t0) * D; e += 256) {
-    const float x = load_real(r.p, (row0 + t.t0 + e / D) * r.row + head * r.head + e % D, g.type);
-    const float v = now > 0.f && fabsf(x) <= 3.402823466e38f ? fminf(fmaxf(rintf(x / now), -127.f), 127.f) : 0.f;
-    q[element(g.c, values, t.t0 + e / D, e % D)] = (int8_t)v;
+  if (bad && g.flag != nullptr) *g.flag = 1;
+  __shared__ float part[4];
+  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
+  const float old = t.t0 > 0 ? *scale : 0.f;
+  __syncthreads();  // (every thread has read the old scale)
+  const float now = fmaxf(old, fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) / 127.f);
+  if (threadIdx.x == 0) *scale = now;
+  if (now != old && t.t0 > 0) {
+    // the older tokens on the new scale, 16 bytes at a time: keys' first t0 rows, values' first t0 columns
+    const float ratio = old / now;
+    const int chunks = values ? (t.t0 + 15) / 16 : D / 16, lines = values ? D : t.t0, line = values ? block : D;
+    for (int e = threadIdx.x; e < lines * chunks; e += 256) {
+      const int c = e % chunks;
+      uint4* p = reinterpret_cast<uint4*>(q + (e / chunks) * line + 16 * c);
+      const int keep = values ? t.t0 - 16 * c : 16;  // the bytes after these are not older tokens
+      uint4 w = *p;
+      int8_t* b = reinterpret_cast<int8_t*>(&w);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i < keep) b[i] = (int8_t)fminf(fmaxf(rintf((float)b[i] * ratio), -127.f), 127.f);
+      *p = w;
+    }
+    __syncthreads();  // the rows' bytes share words with these
+  }
+  const int stride = block + 4;
+  for (int e = threadIdx.x; e < pieces; e += 256) {
+    const Any8Of<E> v = piece(e);
+    const int slot = t.t0 + e / per_row, d = 8 * (e % per_row);
+    union {
+      int8_t b[8];
+      uint2 w;
+    } o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.b[i] = quantised((float)v.v[i], now);
+    if (!values) {
+      *reinterpret_cast<uint2*>(q + slot * D + d) = o.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turned[(d + i) * stride + slot] = (uint8_t)o.b[i];
+    }
+  }
+  if (!values) return;
+  __syncthreads();
+  if (t.t0 == 0 && t.t1 == block) {
+    for (int e = threadIdx.x; e < D * block / 16; e += 256) {
+      const int d = e / (block / 16), c = e % (block / 16);
+      const uint32_t* w = reinterpret_cast<const uint32_t*>(turned + d * stride + 16 * c);
+      reinterpret_cast<uint4*>(q)[e] = uint4{w[0], w[1], w[2], w[3]};
+    }
+  } else {
+    const int n = t.t1 - t.t0;
+    for (int e = threadIdx.x; e < D * n; e += 256) q[e / n * block + t.t0 + e % n] = (int8_t)turned[e / n * stride + t.t0 + e % n];
   }
 }
 
-__global__ __launch_bounds__(256) void load_plain_kernel(CacheLaunch g) {
-  const Tile t = tile_of(g, g.flag);
+template <class E>
+__global__ __launch_bounds__(256) void load_kernel(CacheLaunch g) {
+  const Tile t = tile_of(g);
   if (t.id < 0) return;
   const bool values = blockIdx.z & 1;
-  const int head = blockIdx.y, D = g.c.head_dim;
+  const int head = blockIdx.y, D = g.c.head_dim, block = g.c.block, per_row = D / 8, stride = block + 4;
   const Rows& r = values ? g.v : g.k;
   const int64_t at = (int64_t)t.id * g.c.heads + head;
-  const int8_t* q = (values ? g.c.v : g.c.k) + at * g.c.block * D;
+  const int8_t* q = (values ? g.c.v : g.c.k) + at * block * D;
   const float scale = (values ? g.c.v_scales : g.c.k_scales)[at];
-  const int64_t row0 = t.s.row0 + (t.first - (t.s.len - t.s.rows));
-  for (int e = threadIdx.x; e < (t.t1 - t.t0) * D; e += 256)
-    store_real(r.p, (row0 + t.t0 + e / D) * r.row + head * r.head + e % D, g.type,
-               (float)q[element(g.c, values, t.t0 + e / D, e % D)] * scale);
+  E* rows = reinterpret_cast<E*>(r.p) + t.row0 * r.row + head * r.head;
+  if (values) {
+    const int c0 = t.t0 / 16, chunks = (t.t1 + 15) / 16 - c0;  // those that hold the slots
+    for (int e = threadIdx.x; e < D * chunks; e += 256) {
+      const int d = e / chunks, c = c0 + e % chunks;
+      const uint4 w = *reinterpret_cast<const uint4*>(q + d * block + 16 * c);
+      uint32_t* p = reinterpret_cast<uint32_t*>(turned + d * stride + 16 * c);
+      p[0] = w.x, p[1] = w.y, p[2] = w.z, p[3] = w.w;
+    }
+    __syncthreads();
+  }
+  for (int e = threadIdx.x; e < (t.t1 - t.t0) * per_row; e += 256) {
+    const int slot = t.t0 + e / per_row, d = 8 * (e % per_row);
+    union {
+      int8_t b[8];
+      uint2 w;
+    } o;
+    if (!values) {
+      o.w = *reinterpret_cast<const uint2*>(q + slot * D + d);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o.b[i] = (int8_t)turned[(d + i) * stride + slot];
+    }
+    Any8Of<E> v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v.v[i] = (E)((float)o.b[i] * scale);
+    *reinterpret_cast<Any8Of<E>*>(rows + slot * r.row + d) = v;
+  }
 }
 
 // ---- attention ------------------------------------------------------------------------------
@@ -152,7 +222,7 @@ __device__ __forceinline__ int64_t part_index(const AttendArgs& a, int s, int h,
   return ((((int64_t)s * a.g.c.heads + h) * cols + c) * a.splits + x) * (D + 4);
 }
 
-// A row's element type, and eight elements from any address.
+// A row's element type.
 template <awe_dtype T>
 struct RowType;
 template <>
@@ -163,11 +233,6 @@ template <>
 struct RowType<AWE_F16> {
   using Elem = _Float16;
 };
-template <class E>
-struct __attribute__((packed)) Any8Of {
-  E v[8];
-};
-
 // What a wave keeps of its 16 kQ columns: queries, running maximum, weights' sum and weighted values.
 template <awe_dtype T, int D, int kQ>
 struct Columns {
@@ -583,15 +648,17 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
   }
 }
 
-// Joins the splits of a column: a workgroup per column, whose waves take the splits in turn (D / 64
-// dimensions per lane), eight at a time in flight.
+// Joins the splits of a column, D / 64 dimensions per lane, eight splits at a time in flight: a wave per
+// column, or where there are more splits the waves of a workgroup, in turn.
+constexpr int kJoinAlone = 16;
 template <awe_dtype T, int D>
 __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a) {
   using Elem = typename RowType<T>::Elem;
   constexpr int kAtOnce = 8;
   const int sid = blockIdx.z, head = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Seq s = sequence(a.g.b, sid, false, nullptr, false);
-  const int64_t col = blockIdx.x;
+  const bool alone = a.splits <= kJoinAlone;
+  const int64_t col = alone ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x;
   if (s.len <= a.chunk || col >= (int64_t)s.rows * a.share) return;
   const int n = (s.len + a.chunk - 1) / a.chunk;
   const float* p = a.part + part_index(a, sid, head, col, 0, D);
@@ -600,11 +667,12 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a) 
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   const float base = top == -INFINITY ? 0.f : top;
   float sum = 0.f, v[D / 64] = {};
-  for (int x0 = wave; x0 < n; x0 += kWaves * kAtOnce) {
+  const int in_turn = alone ? 1 : kWaves;
+  for (int x0 = alone ? 0 : wave; x0 < n; x0 += in_turn * kAtOnce) {
     float m[kAtOnce], l[kAtOnce], o[kAtOnce][D / 64];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      const int x = x0 + u * kWaves;
+      const int x = x0 + u * in_turn;
       const float* px = p + (int64_t)(x < n ? x : x0) * (D + 4);
       m[u] = x < n ? px[0] : -INFINITY;
       l[u] = px[1];
@@ -613,20 +681,24 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a) 
     }
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      if (x0 + u * kWaves >= n) break;
+      if (x0 + u * in_turn >= n) break;
       const float f = __builtin_amdgcn_exp2f(m[u] - base);
       sum += l[u] * f;
 #pragma unroll
       for (int d = 0; d < D / 64; ++d) v[d] += o[u][d] * f;
     }
   }
+  Elem* out = result<Elem>(a, s, head, col);
+  if (alone) {
+#pragma unroll
+    for (int d = 0; d < D / 64; ++d) out[64 * d + lane] = (Elem)(sum == 0.f ? 0.f : v[d] / sum);
+    return;
+  }
   __shared__ float parts[kWaves][D + 1];
 #pragma unroll
   for (int d = 0; d < D / 64; ++d) parts[wave][64 * d + lane] = v[d];
   if (lane == 0) parts[wave][D] = sum;
   __syncthreads();
-  Elem* out = reinterpret_cast<Elem*>(a.g.o.p) + (int64_t)(s.row0 + col / a.share) * a.g.o.row +
-              (head * a.share + col % a.share) * a.g.o.head;
   for (int d = threadIdx.x; d < D; d += 64 * kWaves) {
     float t = 0.f, w = 0.f;
 #pragma unroll
@@ -641,7 +713,8 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a) 
 // Grid (blocks that can be touched, heads, 2 * sequences); sequences go over in parts of the grid's limit.
 template <class K>
 awe_status launch_tiles(K kernel, CacheLaunch g, const char* what, hipStream_t stream) {
-  const unsigned x = (unsigned)((g.b.max_rows + g.c.block - 1) / g.c.block + 1);
+  // n rows touch at most 1 + ceil((n - 1) / block) blocks
+  const unsigned x = (unsigned)((std::min(g.b.max_rows, g.b.rows) + g.c.block - 2) / g.c.block + 1);
   const int32_t all = g.b.sequences;
   for (int32_t s = 0; s < all; s += 32767) {
     CacheLaunch part = g;
@@ -649,7 +722,7 @@ awe_status launch_tiles(K kernel, CacheLaunch g, const char* what, hipStream_t s
     part.b.starts += s;
     part.b.lengths += s;
     part.b.blocks += s * g.b.ld_blocks;
-    hipLaunchKernelGGL(kernel, dim3(x, (unsigned)g.c.heads, 2u * part.b.sequences), dim3(256), 0, stream, part);
+    hipLaunchKernelGGL(kernel, dim3(x, (unsigned)g.c.heads, 2u * part.b.sequences), dim3(256), turned_bytes(g.c), stream, part);
     const awe_status st = launched(what);
     if (st != AWE_OK) return st;
   }
@@ -659,11 +732,17 @@ awe_status launch_tiles(K kernel, CacheLaunch g, const char* what, hipStream_t s
 }  // namespace
 
 awe_status launch_cache_store(const CacheLaunch& g, hipStream_t stream) {
-  return launch_tiles(store_plain_kernel, g, "cache store launch", stream);
+  const char* what = "cache store launch";
+  return g.type == AWE_F32    ? launch_tiles(store_kernel<float>, g, what, stream)
+         : g.type == AWE_BF16 ? launch_tiles(store_kernel<bf16>, g, what, stream)
+                              : launch_tiles(store_kernel<f16>, g, what, stream);
 }
 
 awe_status launch_cache_load(const CacheLaunch& g, hipStream_t stream) {
-  return launch_tiles(load_plain_kernel, g, "cache load launch", stream);
+  const char* what = "cache load launch";
+  return g.type == AWE_F32    ? launch_tiles(load_kernel<float>, g, what, stream)
+         : g.type == AWE_BF16 ? launch_tiles(load_kernel<bf16>, g, what, stream)
+                              : launch_tiles(load_kernel<f16>, g, what, stream);
 }
 
 namespace {
@@ -685,7 +764,7 @@ awe_status launch_attend(const AttendArgs& a, bool own_columns, hipStream_t stre
   awe_status st = launched("attention launch");
   if (st != AWE_OK || a.splits == 1) return st;
   const int64_t cols = a.g.b.max_rows * a.share;
-  hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)cols, heads, seqs), block, 0, stream, a);
+  hipLaunchKernelGGL((attend_join_kernel<T, D>), dim3((unsigned)(a.splits <= kJoinAlone ? (cols + kWaves - 1) / kWaves : cols), heads, seqs), block, 0, stream, a);
   return launched("attention join launch");
 }
 }  // namespace
