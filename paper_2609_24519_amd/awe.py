@@ -367,13 +367,17 @@ def matmul_crt(A, B, moduli, bound_a, bound_b, d_range_flag=None):
 
 
 # ---- quantised inference on torch tensors ------------------------------------------------------
-_types = {}  # torch dtype -> awe_dtype, filled when torch is first needed
+_types = {}  # torch dtype -> awe_dtype
+_torch = None  # both set when torch is first needed
 
 
 def _dtype(t, allowed):
-    if not _types:
+    global _torch
+    if _torch is None:
         import torch
-        _types.update({torch.int8: I8, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+        _types.update({torch.int8: I8, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16,
+                       torch.int32: I32})
+        _torch = torch
     code = _types.get(t)
     if code not in allowed:
         raise ValueError("element type %s is not supported here" % t)
@@ -382,51 +386,62 @@ def _dtype(t, allowed):
 
 def _on_current_device(*tensors):
     """The library launches on the current device: its tensors must be there."""
-    import torch
-    here = torch.cuda.current_device()
+    here = -1
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != here):
-            raise ValueError("a tensor is not on the current device (cuda:%d)" % here)
+        if t is None:
+            continue
+        at = t.get_device()
+        if at >= 0 and here < 0:
+            _current_stream()  # initialises CUDA the first time
+            here = _torch_c._cuda_getDevice() if _torch_c is not None else at
+        if at != here or at < 0:
+            raise ValueError("a tensor is not on the current device")
 
 
 def _rows_2d(t, what):
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError("%s must be a matrix with adjacent elements in its rows" % what)
-    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
-        raise ValueError("rows of %s share memory" % what)
-    return max(t.stride(0), t.shape[1])  # a single row may have any stride
+    """Leading dimension of a matrix with adjacent elements in its rows (a single row may have any stride)."""
+    if t.dim() != 2:
+        raise ValueError("%s must be a matrix" % what)
+    (rows, cols), (ld, one) = t.shape, t.stride()
+    if (one != 1 and cols > 1) or (ld < cols and rows > 1):
+        raise ValueError("%s must have adjacent elements in its rows, and rows that share no memory" % what)
+    return ld if ld > cols else cols
 
 
 def matmul_w4(x, w, scales, group, zeros=None, x_scales=None, out_dtype=None):
     """Y = X W^T for CUDA tensors: x (M x K, bfloat16, float16 or int8), w (N x ceil(K / 2), uint8, two
     codes per byte, the low nibble first), scales and zeros (N x ceil(K / group); zeros uint8 or None
     for 8), x_scales (M float32, int8 x only).  out_dtype: x's type, bfloat16 for int8, if not given."""
-    import torch
-    if x.dim() != 2 or w.dim() != 2 or scales.dim() != 2:
-        raise ValueError("x, w and scales must be matrices")
+    ldx, ldw, lds = _rows_2d(x, "x"), _rows_2d(w, "w"), _rows_2d(scales, "scales")
     M, K = x.shape
-    N = w.shape[0]
+    N, packed = w.shape
     if group <= 0:
         raise ValueError("group must be positive")
     groups = -(-K // group)
     x_type = _dtype(x.dtype, (BF16, F16, I8))
     s_type = _dtype(scales.dtype, (F32, BF16, F16))
-    out_dtype = out_dtype or (torch.bfloat16 if x_type == I8 else x.dtype)
+    if out_dtype is None:
+        out_dtype = _torch.bfloat16 if x_type == I8 else x.dtype
     y_type = _dtype(out_dtype, (F32, BF16, F16))
-    if w.dtype != torch.uint8 or w.shape[1] != (K + 1) // 2:
+    if w.dtype != _torch.uint8 or packed != (K + 1) // 2:
         raise ValueError("w must be uint8 of N x ceil(K / 2)")
-    if tuple(scales.shape) != (N, groups) or (zeros is not None and tuple(zeros.shape) != (N, groups)):
-        raise ValueError("scales and zeros must be N x ceil(K / group)")
-    if zeros is not None and zeros.dtype != torch.uint8:
-        raise ValueError("zeros must be uint8")
-    if x_scales is not None and (x_scales.dtype != torch.float32 or tuple(x_scales.shape) != (M,)
+    if scales.shape != (N, groups):
+        raise ValueError("scales must be N x ceil(K / group)")
+    ldz = 0
+    if zeros is not None:
+        ldz = _rows_2d(zeros, "zeros")
+        if zeros.dtype != _torch.uint8 or zeros.shape != (N, groups):
+            raise ValueError("zeros must be uint8 of N x ceil(K / group)")
+    if x_scales is not None and (x_scales.dtype != _torch.float32 or x_scales.shape != (M,)
                                  or not x_scales.is_contiguous()):
         raise ValueError("x_scales must be M float32 values")
     _on_current_device(x, w, scales, zeros, x_scales)
-    y = torch.empty((M, N), dtype=out_dtype, device=x.device)
-    gemm_w4(M, N, K, x, _rows_2d(x, "x"), x_type, x_scales, w, _rows_2d(w, "w"), scales, _rows_2d(scales, "scales"),
-            s_type, zeros, 0 if zeros is None else _rows_2d(zeros, "zeros"), group, y, N, y_type)
+    y = x.new_empty((M, N), dtype=out_dtype)
+    gemm_w4(M, N, K, x, ldx, x_type, x_scales, w, ldw, scales, lds, s_type, zeros, ldz, group, y, N, y_type)
     return y
+
+
+_INT8, _INT32, _FLOAT32 = (I8,), (I32,), (F32,)
 
 
 class Cache:
@@ -435,14 +450,13 @@ class Cache:
     the tensors alive; ``Cache.empty`` allocates them."""
 
     def __init__(self, k, v, k_scales, v_scales):
-        import torch
         if k.dim() != 4 or v.dim() != 4:
             raise ValueError("k and v have four dimensions")
         blocks, heads, block, dim = k.shape
-        if tuple(v.shape) != (blocks, heads, dim, block) or k.dtype != torch.int8 or v.dtype != torch.int8:
+        if v.shape != (blocks, heads, dim, block) or _dtype(k.dtype, _INT8) != _dtype(v.dtype, _INT8):
             raise ValueError("k must be int8 of blocks x heads x block x dim, v of blocks x heads x dim x block")
         for s in (k_scales, v_scales):
-            if tuple(s.shape) != (blocks, heads) or s.dtype != torch.float32:
+            if s.shape != (blocks, heads) or _dtype(s.dtype, _FLOAT32) != F32:
                 raise ValueError("scales must be float32 of blocks x heads")
         for t in (k, v, k_scales, v_scales):
             if not t.is_contiguous():
@@ -467,12 +481,10 @@ class Batch:
     (the rows of the row tensors, and bounds).  Keeps the tensors alive."""
 
     def __init__(self, starts, lengths, blocks, rows, max_rows, max_length):
-        import torch
         n = lengths.shape[0]
         for t in (starts, lengths, blocks):
-            if t.dtype != torch.int32:
-                raise ValueError("starts, lengths and blocks must be int32")
-        if tuple(starts.shape) != (n + 1,) or lengths.dim() != 1 or blocks.dim() != 2 or blocks.shape[0] != n:
+            _dtype(t.dtype, _INT32)
+        if starts.shape != (n + 1,) or lengths.dim() != 1 or blocks.dim() != 2 or blocks.shape[0] != n:
             raise ValueError("starts, lengths and blocks must have sequences + 1, sequences and sequences rows")
         if not starts.is_contiguous() or not lengths.is_contiguous():
             raise ValueError("starts and lengths must be contiguous")
@@ -486,10 +498,11 @@ class Batch:
 
 
 def _row_tensor(t, cache, batch, heads, what):
-    if t.dim() != 3 or tuple(t.shape) != (batch.rows, heads, cache.head_dim) or t.stride(2) != 1:
+    stride = t.stride()
+    if t.shape != (batch.rows, heads, cache.head_dim) or stride[2] != 1:
         raise ValueError("%s must be rows x %d x %d with adjacent elements in the last dimension"
                          % (what, heads, cache.head_dim))
-    return t.stride(0), t.stride(1)
+    return stride[0], stride[1]
 
 
 def _fits(cache, batch):
@@ -524,19 +537,18 @@ def load_tokens(cache, batch, dtype, d_range_flag=None):
 def attend(cache, batch, q, scale, causal=True, out=None, d_range_flag=None):
     """Attention of q (rows x query heads x dim) over the cached tokens of the batch's sequences.  Rows that
     belong to no sequence are not written."""
-    import torch
     _fits(cache, batch)
     heads = q.shape[1] if q.dim() == 3 else 0
     q_row, q_head = _row_tensor(q, cache, batch, heads, "q")
     dtype = _dtype(q.dtype, (BF16, F16))
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     elif out.dtype != q.dtype:
         raise ValueError("out and q have different types")
     out_row, out_head = _row_tensor(out, cache, batch, heads, "out")
     _on_current_device(cache.k, batch.starts, q, out)
     n = cache_attend_workspace_bytes(cache, batch, heads)
-    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    ws = q.new_empty(n, dtype=_torch.uint8) if n else None
     cache_attend(cache, batch, q, q_row, q_head, heads, dtype, scale, 1 if causal else 0, out, out_row, out_head, ws,
                  n, d_range_flag)
     return out
