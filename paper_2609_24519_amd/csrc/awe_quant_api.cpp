@@ -29,6 +29,8 @@ bool aligned(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(
 constexpr int64_t kMost = 0x7fffff00LL;        // sizes of a product, tokens and blocks of a cache
 constexpr int64_t kMostRows = int64_t(1) << 27;  // rows of a batch (they span the grid)
 constexpr int64_t kMostStride = int64_t(1) << 40;
+// Bytes from one row of a product's operand to the next: the kernels reach a tile's 256 rows by 32 bits.
+constexpr int64_t kMostRow = int64_t(1) << 24;
 
 awe_status w4_impl(const W4Launch& g, hipStream_t stream) {
   if (g.M < 0 || g.N < 0 || g.K < 0) return invalid("negative size");
@@ -47,6 +49,9 @@ awe_status w4_impl(const W4Launch& g, hipStream_t stream) {
     if (g.x == nullptr || g.w == nullptr || g.scales == nullptr) return invalid("X, W or w_scales is NULL");
     if (g.ldx < g.K || g.ldw < (g.K + 1) / 2 || g.lds < groups || (g.zeros != nullptr && g.ldz < groups))
       return invalid("leading dimension too small");
+    if (g.ldx * elem_bytes(g.x_type) >= kMostRow || g.ldw >= kMostRow || g.lds * elem_bytes(g.s_type) >= kMostRow ||
+        (g.zeros != nullptr && g.ldz >= kMostRow))
+      return refuse(AWE_ERR_UNSUPPORTED, "rows of an operand too far apart");
     if (!aligned(g.x, elem_bytes(g.x_type)) || !aligned(g.scales, elem_bytes(g.s_type)) || !aligned(g.x_scales, 4))
       return invalid("an operand is not aligned to its element");
   }

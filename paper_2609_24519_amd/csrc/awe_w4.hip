@@ -376,7 +376,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 
 // Many rows: a workgroup has 16 kM rows and 64 kN outputs, 16 kN of them each of its four waves, and goes
 // through the reduction chunk by chunk.  The rows of X lie in LDS, twice (one chunk is multiplied while the
-// next one is fetched and put in the order of the codes), together with what the codes' bias makes of each
+// next one is put there in the order of the codes, and the one after that is on its way), together with what the codes' bias makes of each
 // row, -(bias + 8) sum x over a group, which is where a group's sum starts; scales and zero points lie there
 // too, as floats.  A wave's weights go from memory to its registers, and no other wave unpacks them.
 // kG groups of four waves take the chunks in turn, each with X of its own in LDS, and add up at the end, so that
@@ -428,13 +428,16 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
 
   // this thread's part of the fetching: pieces first .. first + kPieces - 1 of a row, and the scale of an output
   const int my_row = tid / kPer, first = tid % kPer * kPieces;
-  const Elem* xp = reinterpret_cast<const Elem*>(g.x) + std::min<int64_t>(m0 + my_row, g.M - 1) * g.ldx;
-  const int64_t my_col = std::min<int64_t>(n0 + tid, g.N - 1);
+  const uint8_t* xb = reinterpret_cast<const uint8_t*>(g.x) + m0 * g.ldx * kE;
+  const uint32_t xo = ((uint32_t)std::min<int64_t>(my_row, g.M - 1 - m0) * (uint32_t)g.ldx + 8 * first) * kE;
   const int32_t full = (int32_t)(g.K / kChunk), chunks = (int32_t)((g.K + kChunk - 1) / kChunk);
   const int32_t last = (int32_t)((g.K - 1) / g.group);
   const bool has_z = g.zeros != nullptr;
-  const uint8_t* zb = has_z ? g.zeros : g.w;  // (any byte, where there are none)
   const int s_shift = g.s_type == AWE_F32 ? 2 : 1;
+  const uint32_t my_col = (uint32_t)std::min<int64_t>(tid, g.N - 1 - n0);
+  const uint8_t* sb = reinterpret_cast<const uint8_t*>(g.scales) + ((n0 * g.lds) << s_shift);
+  const uint8_t* zb = has_z ? g.zeros + n0 * g.ldz : g.w;  // (any byte, where there are none)
+  const uint32_t so = (my_col * (uint32_t)g.lds) << s_shift, zo = has_z ? my_col * (uint32_t)g.ldz : 0;
   struct Fetched {
     Raw x[kPieces];
     uint32_t s[kSub], z[kSub];  // as they lie in memory: nothing may wait for them here
@@ -442,15 +445,15 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
   auto fetch = [&](Fetched& f, int32_t c, bool end) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      const int64_t k = (int64_t)c * kChunk + 8 * (first + p);
-      f.x[p] = end ? load8_end<T>(xp, k, g.K) : load8<T>(xp + k);
+      f.x[p] = end ? load8_end<T>(reinterpret_cast<const Elem*>(xb + (xo - 8 * first * kE)), (int64_t)c * kChunk + 8 * (first + p), g.K)
+                   : load8<T>(reinterpret_cast<const Elem*>(xb + ((int64_t)c * kChunk + 8 * p) * kE + xo));
     }
 #pragma unroll
     for (int j = 0; j < kSub; ++j) {
       const int32_t grp = std::min((int32_t)((uint32_t)(kFine ? 4 * c + j : c) / (uint32_t)a.units), last);
-      const uint8_t* s = reinterpret_cast<const uint8_t*>(g.scales) + ((my_col * g.lds + grp) << s_shift);
+      const uint8_t* s = sb + (so + ((uint32_t)grp << s_shift));
       f.s[j] = s_shift == 2 ? raw_scale<AWE_F32>(s) : raw_scale<AWE_F16>(s);
-      f.z[j] = zb[has_z ? my_col * g.ldz + grp : 0];
+      f.z[j] = zb[zo + (has_z ? (uint32_t)grp : 0)];
     }
   };
   auto keep = [&](const Fetched& f, int buf) {
@@ -513,7 +516,7 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
 #pragma unroll
     for (int u = 0; u < kM; ++u) acc[t][u] = f4{0.f, 0.f, 0.f, 0.f};
 
-  auto multiply = [&](u4 (&now)[kN], int buf, auto between) {
+  auto multiply = [&](u4 (&now)[kN], int buf) {
     Acc part[kN][kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -533,7 +536,6 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
 #pragma unroll
         for (int u = 0; u < kM; ++u) part[t][u] = X::mul(e[u], op, begin ? start[u] : part[t][u]);
       }
-      if (j == 0) between();
       if (!kFine && j < 3) continue;
 #pragma unroll
       for (int t = 0; t < kN; ++t) {
@@ -568,19 +570,19 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
       codes(now, group, false);
       fetch(f, group, false);
       keep(f, 0);
+      if (group + kG < full) fetch(f, group + kG, false);
     }
 #pragma unroll 1
     for (int32_t st = 0; st < stages; ++st) {
       const int32_t c = kG * st + group;
       __syncthreads();  // chunk c is there, and nobody reads the other half any more
       if (c < full) {
-        multiply(now, st & 1, [&] {
-          if (c + kG < full) {
-            codes(ahead, c + kG, false);
-            fetch(f, c + kG, false);
-          }
-        });
-        if (c + kG < full) keep(f, (st & 1) ^ 1);
+        if (c + kG < full) {
+          codes(ahead, c + kG, false);
+          keep(f, (st & 1) ^ 1);
+        }
+        if (c + 2 * kG < full) fetch(f, c + 2 * kG, false);
+        multiply(now, st & 1);
       }
 #pragma unroll
       for (int t = 0; t < kN; ++t) now[t] = ahead[t];
@@ -595,7 +597,7 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
       keep(f, stages & 1);
     }
     __syncthreads();
-    if (group == full % kG) multiply(now, stages & 1, [] {});
+    if (group == full % kG) multiply(now, stages & 1);
   }
   if (kG > 1) {
     float* part = reinterpret_cast<float*>(tile_lds);
@@ -665,8 +667,10 @@ awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
     return AWE_ERR_UNSUPPORTED;
   }
   // the widest tile that still gives each of the 256 CUs one; two workgroups per CU where there are enough
-  if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFine>(a, tiles(256), stream);
-  if (tiles(256) >= 256) return launch_tile<T, 4, 4, 2, kFine>(a, tiles(256), stream);
+  if constexpr (!kFine) {  // (a fold at every step needs more registers than such a tile leaves)
+    if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFine>(a, tiles(256), stream);
+    if (tiles(256) >= 256) return launch_tile<T, 4, 4, 2, kFine>(a, tiles(256), stream);
+  }
   if (tiles(128) >= 256) return launch_tile<T, 4, 2, 2, kFine>(a, tiles(128), stream);
   return launch_tile<T, 4, 1, 2, kFine>(a, tiles(64), stream);
 }
