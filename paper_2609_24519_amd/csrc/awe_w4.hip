@@ -155,7 +155,7 @@ constexpr int kChunk = 128;  // reduction indices of a wave's step: 16 bytes of 
 
 struct W4Args {
   W4Launch g;
-  int32_t units;      // group / 128, or group / 32 where 128 does not divide it
+  int32_t units;  // group / 128, or group / 64 or / 32 where 128 does not divide it
 };
 
 // A lane loads row n of W at indices 32 q .. 32 q + 31 of the chunk (16 bytes); the words are then transposed over
@@ -220,11 +220,12 @@ __device__ __forceinline__ float scale_value(uint32_t raw) {
 // 10.6 for one row at 8192 x 8192; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
 constexpr int kW = 8;
 
-template <awe_dtype T, int kM, int kN, int kD, bool kFine, awe_dtype S>
+template <awe_dtype T, int kM, int kN, int kD, int kFold, awe_dtype S>
 __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   using X = Kind<T>;
   using Elem = typename X::Elem;
-  constexpr int kS = kFine ? kD : 1;
+  constexpr int kUnits = 4 / kFold;          // of a chunk
+  constexpr int kS = kFold < 4 ? kD : 1;
   constexpr int kE = sizeof(Elem), kSE = S == AWE_F32 ? 4 : 2;
   const W4Launch& g = a.g;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
@@ -254,8 +255,8 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
     for (int u = 0; u < kM; ++u) acc[t][u] = f4{0.f, 0.f, 0.f, 0.f};
 
-  // A chunk's products.  s, z: a lane's scale and zero point of output tile t, in quarter `of` + step (kFine) or
-  // in quarter `of`.
+  // A chunk's products.  s, z: a lane's scale and zero point of output tile t, in the quarter that fetched
+  // it: the step's, or `of` where a chunk lies in one group.
   auto chunk = [&](const u4 (&cw)[kN], const typename X::Raw (&xr)[kM][4], const uint32_t (&s)[kN], const uint32_t (&z)[kN],
                    int of) {
     u4 c[kN];
@@ -264,7 +265,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
     typename X::Acc part[kN][kM], sum[kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool first = kFine || j == 0;
+      const bool first = j % kFold == 0;
       typename X::Op e[kM];
 #pragma unroll
       for (int u = 0; u < kM; ++u) {
@@ -277,11 +278,11 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
         for (int u = 0; u < kM; ++u) part[t][u] = X::mul(e[u], op, first ? X::zero() : part[t][u]);
       }
-      if (!kFine && j < 3) continue;
+      if (j % kFold != kFold - 1) continue;
       // a group's part: part - (bias + z) sum x, times the group's scale
 #pragma unroll
       for (int t = 0; t < kN; ++t) {
-        const int from = 16 * (kFine ? j : of) + i;
+        const int from = 16 * (kFold < 4 ? j : of) + i;
         const float sc = scale_value<S>(__shfl(s[t], from)), b = X::kBias + (has_z ? (float)__shfl(z[t], from) : 8.f);
 #pragma unroll
         for (int u = 0; u < kM; ++u)
@@ -315,9 +316,9 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
         cw[u][t] = u4{v.w[0], v.w[1], v.w[2], v.w[3]};
       }
     }
-    // quarter q fetches the scales of the q-th chunk (of step q of each, if fine)
+    // quarter q fetches the scales of the q-th chunk (of step q of each, where it has several)
 #pragma unroll
-    for (int v = 0; v < kS; ++v) scales(kFine ? 4 * (c0 + v * kW) + q : c0 + q * kW, s[v], z[v]);
+    for (int v = 0; v < kS; ++v) scales(kFold < 4 ? kUnits * (c0 + v * kW) + q / kFold : c0 + q * kW, s[v], z[v]);
 #pragma unroll
     for (int u = 0; u < kD; ++u) {
       const int64_t c = std::min(c0 + u * kW, full - 1);
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
     for (int u = 0; u < kD; ++u) {
       if (c0 + u * kW >= full) break;
-      chunk(cw[u], xr[u], s[kFine ? u : 0], z[kFine ? u : 0], u);
+      chunk(cw[u], xr[u], s[kFold < 4 ? u : 0], z[kFold < 4 ? u : 0], u);
     }
   }
 
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
         const Elem* row = reinterpret_cast<const Elem*>(xb + (xo[t] - 8 * q * kE));
         xr[t][j] = load8_end<T>(row, k0 + step_offset(q, j), g.K);
       }
-    scales(kFine ? 4 * full + q : full, s, z);
+    scales(kFold < 4 ? kUnits * full + q / kFold : full, s, z);
     chunk(cw, xr, s, z, 0);
   }
 
@@ -381,31 +382,31 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 // too, as floats.  A wave's weights go from memory to its registers, and no other wave unpacks them.
 // kG groups of four waves take the chunks in turn, each with X of its own in LDS, and add up at the end, so that
 // a CU with one workgroup has two waves per SIMD, too.
-template <awe_dtype T, int kM, int kN, bool kFine>
+template <awe_dtype T, int kM, int kN, int kFold>
 struct TileLds {  // of a group of waves
   using X = Kind<T>;
-  static constexpr int kRows = 16 * kM, kCols = 64 * kN, kSub = kFine ? 4 : 1;
+  static constexpr int kRows = 16 * kM, kCols = 64 * kN, kSub = 4 / kFold;
   alignas(16) uint8_t x[2][kRows * kChunk * sizeof(typename X::Elem)];
   alignas(16) typename X::Sum start[2][kSub][kRows], sum[2][kSub][kRows];
   float s[2][kSub][kCols], z[2][kSub][kCols];
 };
-template <awe_dtype T, int kM, int kN, int kG, bool kFine>
+template <awe_dtype T, int kM, int kN, int kG, int kFold>
 constexpr int tile_lds_bytes() {
-  const int groups = kG * (int)sizeof(TileLds<T, kM, kN, kFine>), sums = (kG - 1) * 256 * kM * kN * 16;
+  const int groups = kG * (int)sizeof(TileLds<T, kM, kN, kFold>), sums = (kG - 1) * 256 * kM * kN * 16;
   return groups > sums ? groups : sums;
 }
 
-template <awe_dtype T, int kM, int kN, int kG, bool kFine>
+template <awe_dtype T, int kM, int kN, int kG, int kFold>
 __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
   using X = Kind<T>;
   using Elem = typename X::Elem;
   using Raw = typename X::Raw;
   using Acc = typename X::Acc;
   using Sum = typename X::Sum;
-  constexpr int kE = sizeof(Elem), kRows = 16 * kM, kCols = 64 * kN, kSub = kFine ? 4 : 1;
+  constexpr int kE = sizeof(Elem), kRows = 16 * kM, kCols = 64 * kN, kSub = 4 / kFold;
   constexpr int kPer = 256 / kRows;           // threads that fetch a row
   constexpr int kPieces = kChunk / 8 / kPer;  // pieces of 8 elements each of them has
-  static_assert(kPieces % 4 == 0, "a thread's pieces make up steps of 32 indices");
+  static_assert(kPieces == 4, "a thread's pieces make up a step of 32 indices");
   static_assert(kCols <= 256, "a thread per output fetches its scale");
   const W4Launch& g = a.g;
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
@@ -419,7 +420,7 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
   const int64_t m0 = (8 * band + in % high) * kRows, n0 = in / high * kCols;
 
   extern __shared__ uint8_t tile_lds[];
-  TileLds<T, kM, kN, kFine>& lds = reinterpret_cast<TileLds<T, kM, kN, kFine>*>(tile_lds)[group];
+  TileLds<T, kM, kN, kFold>& lds = reinterpret_cast<TileLds<T, kM, kN, kFold>*>(tile_lds)[group];
   // where a row's piece of 8 elements lies: units of 16 bytes, permuted by the row, so that the same
   // piece of 16 rows lies in different banks
   auto place = [](int row, int piece) {
@@ -450,35 +451,26 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
     }
 #pragma unroll
     for (int j = 0; j < kSub; ++j) {
-      const int32_t grp = std::min((int32_t)((uint32_t)(kFine ? 4 * c + j : c) / (uint32_t)a.units), last);
+      const int32_t grp = std::min((int32_t)((uint32_t)(kSub * c + j) / (uint32_t)a.units), last);
       const uint8_t* s = sb + (so + ((uint32_t)grp << s_shift));
       f.s[j] = s_shift == 2 ? raw_scale<AWE_F32>(s) : raw_scale<AWE_F16>(s);
       f.z[j] = zb[zo + (has_z ? (uint32_t)grp : 0)];
     }
   };
   auto keep = [&](const Fetched& f, int buf) {
-    Sum sum[kPieces / 4] = {};
+    Sum sum = 0;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       const typename X::Op e = X::elems(f.x[p]);
-      sum[p / 4] = X::add(e, sum[p / 4]);
+      sum = X::add(e, sum);
       *reinterpret_cast<typename X::Op*>(lds.x[buf] + place(my_row, first + p)) = e;
     }
-    if (kFine) {
 #pragma unroll
-      for (int p = 0; p < kPieces / 4; ++p) {
-        lds.start[buf][first / 4 + p][my_row] = sum[p] * -(X::kBias + 8);
-        lds.sum[buf][first / 4 + p][my_row] = sum[p];
-      }
-    } else {
-#pragma unroll
-      for (int p = 1; p < kPieces / 4; ++p) sum[0] += sum[p];
-#pragma unroll
-      for (int d = 1; d < kPer; d *= 2) sum[0] += __shfl_xor(sum[0], d);
-      if (first == 0) {
-        lds.start[buf][0][my_row] = sum[0] * -(X::kBias + 8);
-        lds.sum[buf][0][my_row] = sum[0];
-      }
+    for (int d = 1; d < kFold; d *= 2) sum += __shfl_xor(sum, d);
+    const int step = first / 4;  // this thread's
+    if (step % kFold == 0) {
+      lds.start[buf][step / kFold][my_row] = sum * -(X::kBias + 8);
+      lds.sum[buf][step / kFold][my_row] = sum;
     }
     if (tid >= kCols) return;
 #pragma unroll
@@ -520,23 +512,23 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
     Acc part[kN][kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int sub = kFine ? j : 0;
-      const bool begin = kFine || j == 0;
+      const int sub = j / kFold;
+      const bool begin = j % kFold == 0;
       typename X::Op e[kM];
       Acc start[kM];
 #pragma unroll
       for (int u = 0; u < kM; ++u) {
-        e[u] = *reinterpret_cast<const typename X::Op*>(lds.x[buf] + place(16 * u + i, kFine ? 4 * j + q : 4 * q + j));
+        e[u] = *reinterpret_cast<const typename X::Op*>(lds.x[buf] + place(16 * u + i, kFold < 4 ? 4 * j + q : 4 * q + j));
         if (begin) start[u] = *reinterpret_cast<const Acc*>(&lds.start[buf][sub][16 * u + 4 * q]);
       }
 #pragma unroll
       for (int t = 0; t < kN; ++t) {
-        if (kFine && j == 0) now[t] = across_quarters(now[t]);
+        if (kFold < 4 && j == 0) now[t] = across_quarters(now[t]);
         const typename X::Op op = X::codes(now[t][j], magic);
 #pragma unroll
         for (int u = 0; u < kM; ++u) part[t][u] = X::mul(e[u], op, begin ? start[u] : part[t][u]);
       }
-      if (!kFine && j < 3) continue;
+      if (j % kFold != kFold - 1) continue;
 #pragma unroll
       for (int t = 0; t < kN; ++t) {
         const int col = 16 * (kN * wave + t) + i;
@@ -632,34 +624,34 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
     }
 }
 
-template <awe_dtype T, int kM, int kN, int kD>
-awe_status launch_rows(const W4Args& a, bool fine, hipStream_t stream) {
+template <awe_dtype T, int kFold, int kM, int kN, int kD>
+awe_status launch_rows(const W4Args& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.g.N + 16 * kN - 1) / (16 * kN)), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM)));
   const dim3 block(64 * kW);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
   if (a.g.s_type == AWE_F32)
-    fine ? launch(w4_rows_kernel<T, kM, kN, kD, true, AWE_F32>) : launch(w4_rows_kernel<T, kM, kN, kD, false, AWE_F32>);
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F32>);
   else if (a.g.s_type == AWE_BF16)
-    fine ? launch(w4_rows_kernel<T, kM, kN, kD, true, AWE_BF16>) : launch(w4_rows_kernel<T, kM, kN, kD, false, AWE_BF16>);
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_BF16>);
   else
-    fine ? launch(w4_rows_kernel<T, kM, kN, kD, true, AWE_F16>) : launch(w4_rows_kernel<T, kM, kN, kD, false, AWE_F16>);
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F16>);
   return launched("w4 launch");
 }
 
-template <awe_dtype T, int kM, int kN, int kG, bool kFine>
+template <awe_dtype T, int kM, int kN, int kG, int kFold>
 awe_status launch_tile(const W4Args& a, int64_t tiles, hipStream_t stream) {
   static std::mutex mu;
   static std::set<int> done;
-  constexpr int bytes = tile_lds_bytes<T, kM, kN, kG, kFine>();
+  constexpr int bytes = tile_lds_bytes<T, kM, kN, kG, kFold>();
   static_assert(kG <= 2 && bytes <= 160 * 1024 / (3 - kG), "the workgroups of a CU fit its LDS");
-  auto kernel = w4_tile_kernel<T, kM, kN, kG, kFine>;
+  auto kernel = w4_tile_kernel<T, kM, kN, kG, kFold>;
   const awe_status st = set_lds_limit(reinterpret_cast<const void*>(kernel), bytes, mu, done);
   if (st != AWE_OK) return st;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256 * kG), bytes, stream, a);
   return launched("w4 launch");
 }
 
-template <awe_dtype T, bool kFine>
+template <awe_dtype T, int kFold>
 awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
   auto tiles = [&](int cols) { return ((a.g.M + 63) / 64) * ((a.g.N + cols - 1) / cols); };
   if (tiles(64) > 0xffffff) {
@@ -667,33 +659,39 @@ awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
     return AWE_ERR_UNSUPPORTED;
   }
   // the widest tile that still gives each of the 256 CUs one; two workgroups per CU where there are enough
-  if constexpr (!kFine) {  // (a fold at every step needs more registers than such a tile leaves)
-    if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFine>(a, tiles(256), stream);
-    if (tiles(256) >= 256) return launch_tile<T, 4, 4, 2, kFine>(a, tiles(256), stream);
+  if constexpr (kFold > 1) {  // (a fold at every step needs more registers than such a tile leaves)
+    if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFold>(a, tiles(256), stream);
+    if (tiles(256) >= 256) return launch_tile<T, 4, 4, 2, kFold>(a, tiles(256), stream);
   }
-  if (tiles(128) >= 256) return launch_tile<T, 4, 2, 2, kFine>(a, tiles(128), stream);
-  return launch_tile<T, 4, 1, 2, kFine>(a, tiles(64), stream);
+  if (tiles(128) >= 256) return launch_tile<T, 4, 2, 2, kFold>(a, tiles(128), stream);
+  return launch_tile<T, 4, 1, 2, kFold>(a, tiles(64), stream);
 }
 
-template <awe_dtype T>
-awe_status launch_kind(const W4Args& a, bool fine, hipStream_t stream) {
-  if (a.g.M <= 16) return launch_rows<T, 1, 2, 4>(a, fine, stream);
-  if (a.g.M <= 64) return launch_rows<T, 2, 2, 2>(a, fine, stream);
-  return fine ? launch_tiles<T, true>(a, stream) : launch_tiles<T, false>(a, stream);
+template <awe_dtype T, int kFold>
+awe_status launch_kind(const W4Args& a, hipStream_t stream) {
+  if (a.g.M <= 16) return launch_rows<T, kFold, 1, 2, 4>(a, stream);
+  if (a.g.M <= 64) return launch_rows<T, kFold, 2, 2, 2>(a, stream);
+  return launch_tiles<T, kFold>(a, stream);
+}
+
+template <int kFold>
+awe_status launch_type(const W4Args& a, hipStream_t stream) {
+  if (a.g.x_type == AWE_BF16) return launch_kind<AWE_BF16, kFold>(a, stream);
+  if (a.g.x_type == AWE_F16) return launch_kind<AWE_F16, kFold>(a, stream);
+  return launch_kind<AWE_I8, kFold>(a, stream);
 }
 
 }  // namespace
 
 awe_status launch_w4(const W4Launch& g, hipStream_t stream) {
-  // one group of at least K indices counts as a long one
-  const bool fine = g.group % kChunk != 0 && g.group < g.K;
   W4Args a{};
   a.g = g;
+  // one group of at least K indices counts as one of whole chunks
   if (g.group >= g.K) a.g.group = std::max<int64_t>(1, (g.K + kChunk - 1) / kChunk) * kChunk;
-  a.units = (int32_t)(a.g.group / (fine ? 32 : kChunk));
-  if (g.x_type == AWE_BF16) return launch_kind<AWE_BF16>(a, fine, stream);
-  if (g.x_type == AWE_F16) return launch_kind<AWE_F16>(a, fine, stream);
-  return launch_kind<AWE_I8>(a, fine, stream);
+  // a sum is folded at least every 128 indices, and at every multiple of 32 or 64 where a group may end there
+  const int fold = a.g.group % 128 == 0 ? 4 : a.g.group % 64 == 0 ? 2 : 1;
+  a.units = (int32_t)(a.g.group / (32 * fold));
+  return fold == 4 ? launch_type<4>(a, stream) : fold == 2 ? launch_type<2>(a, stream) : launch_type<1>(a, stream);
 }
 
 }  // namespace awe
