@@ -151,6 +151,16 @@ __device__ __forceinline__ u4 across_quarters(u4 w) {
   return u4{c[0], c[1], d[0], d[1]};
 }
 
+// The same, such that quarter q's words 2 c and 2 c + 1 are the ones at indices 64 c + 16 q .. + 15: sixteen
+// adjacent elements per quarter.
+__device__ __forceinline__ u4 across_quarters_by_16(u4 w) {
+  auto a = __builtin_amdgcn_permlane16_swap(w[0], w[2], false, false);
+  auto b = __builtin_amdgcn_permlane16_swap(w[1], w[3], false, false);
+  auto c = __builtin_amdgcn_permlane32_swap(a[0], a[1], false, false);
+  auto d = __builtin_amdgcn_permlane32_swap(b[0], b[1], false, false);
+  return u4{c[0], d[0], c[1], d[1]};
+}
+
 constexpr int kChunk = 128;  // reduction indices of a wave's step: 16 bytes of codes per lane
 
 struct W4Args {
@@ -161,8 +171,12 @@ struct W4Args {
 // A lane loads row n of W at indices 32 q .. 32 q + 31 of the chunk (16 bytes); the words are then transposed over
 // the quarters, so that step j covers indices 32 j .. 32 j + 31, 8 q .. 8 q + 7 of them in this lane: a step
 // lies in one group (groups begin at multiples of 32 indices), and a load of X's operand reads 64 (int8: 32) adjacent bytes
-// of each row.
-__device__ __forceinline__ int step_offset(int q, int j) { return 32 * j + 8 * q; }
+// of each row.  kPairs (int8 with groups of whole 64s): steps 2 c and 2 c + 1 cover 64 c .. 64 c + 63 between
+// them, 16 adjacent indices in this lane, one load of X.
+template <bool kPairs>
+__device__ __forceinline__ int step_offset(int q, int j) {
+  return kPairs ? 64 * (j >> 1) + 16 * q + 8 * (j & 1) : 32 * j + 8 * q;
+}
 
 // 128 bits, the low word first, shifted right by n < 128.
 __device__ __forceinline__ u4 shifted(u4 v, int n) {
@@ -224,7 +238,8 @@ template <awe_dtype T, int kM, int kN, int kD, int kFold, awe_dtype S>
 __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   using X = Kind<T>;
   using Elem = typename X::Elem;
-  constexpr int kUnits = 4 / kFold;          // of a chunk
+  constexpr int kUnits = 4 / kFold;  // of a chunk
+  constexpr bool kPairs = T == AWE_I8 && kFold > 1;
   constexpr int kS = kFold < 4 ? kD : 1;
   constexpr int kE = sizeof(Elem), kSE = S == AWE_F32 ? 4 : 2;
   const W4Launch& g = a.g;
@@ -247,7 +262,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
     zo[t] = has_z ? n * (uint32_t)g.ldz : 0;
   }
 #pragma unroll
-  for (int t = 0; t < kM; ++t) xo[t] = ((uint32_t)std::min<int64_t>(16 * t + i, g.M - 1 - m0) * (uint32_t)g.ldx + 8 * q) * kE;
+  for (int t = 0; t < kM; ++t) xo[t] = ((uint32_t)std::min<int64_t>(16 * t + i, g.M - 1 - m0) * (uint32_t)g.ldx + step_offset<kPairs>(q, 0)) * kE;
   const uint32_t magic = X::magic();
   f4 acc[kN][kM];
 #pragma unroll
@@ -261,7 +276,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
                    int of) {
     u4 c[kN];
 #pragma unroll
-    for (int t = 0; t < kN; ++t) c[t] = across_quarters(cw[t]);
+    for (int t = 0; t < kN; ++t) c[t] = kPairs ? across_quarters_by_16(cw[t]) : across_quarters(cw[t]);
     typename X::Acc part[kN][kM], sum[kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -325,7 +340,16 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
       for (int t = 0; t < kM; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) xr[u][t][j] = load8<T>(reinterpret_cast<const Elem*>(xb + (c * kChunk + 32 * j) * kE + xo[t]));
+        for (int j = 0; j < 4; ++j) {
+          const uint8_t* p = xb + (c * kChunk + step_offset<kPairs>(0, j)) * kE + xo[t];
+          if constexpr (!kPairs) {
+            xr[u][t][j] = load8<T>(reinterpret_cast<const Elem*>(p));
+          } else if (j % 2 == 0) {
+            const Any16 v = *reinterpret_cast<const Any16*>(p);
+            xr[u][t][j] = (uint64_t)v.w[0] | (uint64_t)v.w[1] << 32;
+            xr[u][t][j + 1] = (uint64_t)v.w[2] | (uint64_t)v.w[3] << 32;
+          }
+        }
     }
 #pragma unroll
     for (int u = 0; u < kD; ++u) {
@@ -346,8 +370,8 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
     for (int t = 0; t < kM; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const Elem* row = reinterpret_cast<const Elem*>(xb + (xo[t] - 8 * q * kE));
-        xr[t][j] = load8_end<T>(row, k0 + step_offset(q, j), g.K);
+        const Elem* row = reinterpret_cast<const Elem*>(xb + (xo[t] - step_offset<kPairs>(q, 0) * kE));
+        xr[t][j] = load8_end<T>(row, k0 + step_offset<kPairs>(q, j), g.K);
       }
     scales(kFold < 4 ? kUnits * full + q / kFold : full, s, z);
     chunk(cw, xr, s, z, 0);
