@@ -14,6 +14,8 @@ v_pk_*_f32 forms.
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -33,26 +35,35 @@ def hipcc():
     return "hipcc"
 
 
-def _compile(sources, lib, verbose):
-    tmp = lib + ".tmp%d" % os.getpid()
-    cmd = [hipcc(), "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-Wall", "-Wno-unused-function",
-           "-I", os.path.join(ROOT, "include")]
-    cmd += [os.path.join(CSRC, s) for s in sources]
-    cmd += ["-o", tmp]
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     out = "\n".join(l for l in res.stdout.splitlines()
                     if "packed-fp32-ops' is not a recognized feature" not in l)
     if res.returncode != 0:
-        if os.path.exists(tmp):
-            os.remove(tmp)
         raise RuntimeError("hipcc failed:\n" + out)
     if verbose and out.strip():
         print(out)
-    os.replace(tmp, lib)
+
+
+def _compile(sources, lib, verbose):
+    """Compiles the sources side by side, four at a time, and links them."""
+    with tempfile.TemporaryDirectory() as td:
+        objects = [os.path.join(td, s + ".o") for s in sources]
+        flags = [hipcc(), "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
+                 "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+                 "-Wall", "-Wno-unused-function", "-I", os.path.join(ROOT, "include")]
+        with ThreadPoolExecutor(4) as pool:
+            list(pool.map(lambda so: _run(flags + ["-c", os.path.join(CSRC, so[0]), "-o", so[1]], verbose),
+                          zip(sources, objects)))
+        tmp = lib + ".tmp%d" % os.getpid()
+        try:
+            _run([hipcc(), "--offload-arch=" + ARCH, "-shared", "-fPIC"] + objects + ["-o", tmp], verbose)
+            os.replace(tmp, lib)
+        finally:
+            if os.path.exists(tmp):
+                os.remove(tmp)
     return lib
 
 
@@ -66,29 +77,29 @@ def kernel_resources():
     (name, vgpr, agpr, sgpr, vgpr spill, sgpr spill, static LDS, scratch, max workgroup) with the
     mangled name's namespace prefix removed."""
     import re
-    import tempfile
 
     import yaml
 
-    rows = []
-    for src in HIP_SOURCES:
+    def metadata(src):
         with tempfile.TemporaryDirectory() as td:
             asm = os.path.join(td, "k.s")
             cmd = [hipcc(), "--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC",
                    "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                    "-I", os.path.join(ROOT, "include"), "--cuda-device-only", "-S",
                    os.path.join(CSRC, src), "-o", asm]
-            res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-            if res.returncode != 0:
-                raise RuntimeError("hipcc failed:\n" + res.stdout)
+            _run(cmd, False)
             text = open(asm).read()
-        meta = text.split(".amdgpu_metadata", 1)[1].split(".end_amdgpu_metadata", 1)[0].replace("\t", " ")
-        for k in yaml.safe_load(meta)["amdhsa.kernels"]:
-            name = re.sub(r"^_ZN3awe12_GLOBAL__N_1", "", k[".name"])
-            rows.append((name, k.get(".vgpr_count"), k.get(".agpr_count"), k.get(".sgpr_count"),
-                         k.get(".vgpr_spill_count"), k.get(".sgpr_spill_count"),
-                         k.get(".group_segment_fixed_size"), k.get(".private_segment_fixed_size"),
-                         k.get(".max_flat_workgroup_size")))
+        return text.split(".amdgpu_metadata", 1)[1].split(".end_amdgpu_metadata", 1)[0].replace("\t", " ")
+
+    rows = []
+    with ThreadPoolExecutor(4) as pool:
+        for meta in pool.map(metadata, HIP_SOURCES):
+            for k in yaml.safe_load(meta)["amdhsa.kernels"]:
+                name = re.sub(r"^_ZN3awe12_GLOBAL__N_1", "", k[".name"])
+                rows.append((name, k.get(".vgpr_count"), k.get(".agpr_count"), k.get(".sgpr_count"),
+                             k.get(".vgpr_spill_count"), k.get(".sgpr_spill_count"),
+                             k.get(".group_segment_fixed_size"), k.get(".private_segment_fixed_size"),
+                             k.get(".max_flat_workgroup_size")))
     return rows
 
 

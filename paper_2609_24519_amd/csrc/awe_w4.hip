@@ -693,9 +693,13 @@ awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
 
 template <awe_dtype T, int kFold>
 awe_status launch_kind(const W4Args& a, hipStream_t stream) {
-  if (a.g.M <= 16) return launch_rows<T, kFold, 1, 2, 4>(a, stream);
-  if (a.g.M <= 64) return launch_rows<T, kFold, 2, 2, 2>(a, stream);
-  return launch_tiles<T, kFold>(a, stream);
+  if (a.g.M > 64) return launch_tiles<T, kFold>(a, stream);
+  // 16 outputs a workgroup while that is at most one per CU (M = 1: 8.4 us instead of 10.4 at 4096 x 8192,
+  // but 12.3 instead of 10.9 at 8192 x 8192); beyond, 32 halve what is read of X
+  const int rows = a.g.M <= 16 ? 16 : 32;
+  const bool narrow = ((a.g.N + 15) / 16) * ((a.g.M + rows - 1) / rows) <= 256;
+  if (rows == 16) return narrow ? launch_rows<T, kFold, 1, 1, 4>(a, stream) : launch_rows<T, kFold, 1, 2, 4>(a, stream);
+  return narrow ? launch_rows<T, kFold, 2, 1, 2>(a, stream) : launch_rows<T, kFold, 2, 2, 2>(a, stream);
 }
 
 template <int kFold>
