@@ -244,6 +244,9 @@ struct Columns {
   f4 o[kQ][D / 16];
   float m[kQ], l[kQ];
   int ev;  // exponent that brings the values' scales seen so far below 1
+  // Weights go into the second product as one FP16 number each where the result is BF16, whose rounding
+  // is eight times coarser, and as two, the number and what its rounding left, where the result is FP16.
+  static constexpr int kParts = T == AWE_F16 ? 2 : 1;
 
   __device__ __forceinline__ void begin(const AttendArgs& a, const Seq& s, int head, int64_t first) {
     const int q4 = (threadIdx.x & 63) >> 4, i16 = threadIdx.x & 15;
@@ -285,7 +288,7 @@ struct Columns {
   // weights.  They lie in one block, so the weights times its values' scale, w = vs 2^(15 - e) < 2^15, are exp2 of
   // one linear function of the scores, and the weights' sum is theirs over w.  FP16 keeps 11 bits of what is
   // at least 2^-29 of the largest scale so far, and to 2^-40 of it of the rest.
-  __device__ __forceinline__ void softmax(f4 (&sc)[kQ][4], h8 (&pf)[kQ][2], bool ok, float ks, float vs, int32_t pv) {
+  __device__ __forceinline__ void softmax(f4 (&sc)[kQ][4], h8 (&pf)[kParts][kQ][2], bool ok, float ks, float vs, int32_t pv) {
     int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
     et = max(et, __shfl_xor(et, 16));
     et = max(et, __shfl_xor(et, 32));
@@ -327,13 +330,15 @@ struct Columns {
         for (int r = 0; r < 4; ++r) {
           const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][b][r], f, shift));
           sum += p;
-          pf[t][b >> 1][4 * (b & 1) + r] = (_Float16)p;
+          const _Float16 high = (_Float16)p;
+          pf[0][t][b >> 1][4 * (b & 1) + r] = high;
+          if constexpr (kParts == 2) pf[1][t][b >> 1][4 * (b & 1) + r] = (_Float16)(p - (float)high);
         }
       l[t] = l[t] * drop + sum * per_w;
       if (__any(!some)) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          if (!some) pf[t][u] = h8{};
+        for (int u = 0; u < 2 * kParts; ++u)
+          if (!some) pf[u >> 1][t][u & 1] = h8{};
       }
       if (__any(keep != 1.f)) {
 #pragma unroll
@@ -461,13 +466,16 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_split_ke
     }
     const float ks0 = ok ? ks : 0.f, vs0 = ok ? vs : 0.f;
     if (t0 + step < to) fetch_keys(t0 + step, ik1);
-    h8 pf[1][2];
+    h8 pf[x.kParts][1][2];
     x.softmax(sc, pf, ok, ks0, vs0, pv);
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-      for (int e = 0; e < 2; ++e)
-        x.o[0][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen(vr[d][2 * e], vr[d][2 * e + 1]), pf[0][e], x.o[0][d], 0, 0, 0);
+      for (int e = 0; e < 2; ++e) {
+        const h8 vf = widen(vr[d][2 * e], vr[d][2 * e + 1]);
+#pragma unroll
+        for (int u = 0; u < x.kParts; ++u) x.o[0][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[u][0][e], x.o[0][d], 0, 0, 0);
+      }
     if (t0 + step < to) {
       fetch_values(t0 + step, iv1);
       iv = iv1;
@@ -622,7 +630,7 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
       }
     }
     reads_ahead<kKeys, kQ>();
-    h8 pf[kQ][2];
+    h8 pf[x.kParts][kQ][2];
     x.softmax(sc, pf, ok, ks0, vs0, pv);
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
@@ -630,9 +638,11 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
       for (int e = 0; e < 2; ++e) {
         const h8 vf = lds[buf][kKeys + 2 * d + e][lane];
 #pragma unroll
-        for (int t = 0; t < kQ; ++t) x.o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][e], x.o[t][d], 0, 0, 0);
+        for (int t = 0; t < kQ; ++t)
+#pragma unroll
+          for (int u = 0; u < x.kParts; ++u) x.o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[u][t][e], x.o[t][d], 0, 0, 0);
       }
-    reads_ahead<kValues, kQ>();
+    reads_ahead<kValues, kQ * x.kParts>();
     if (more) put(buf ^ 1);
   }
   x.end();
