@@ -160,22 +160,29 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
 
 }  // namespace
 
+// Per 64 tokens, a workgroup whose four waves have columns of their own (128 of them) takes 2.0 us while each has a CU
+// to itself and 3.4 us with two on a CU; 16 columns whose tokens are split over waves take 2.2 us of one of 2048 waves.
+// So splitting wins while there are few tiles of 16 columns (measured, 8 heads of 128: 8 sequences of 2048 tokens,
+// 64 columns each 32 us instead of 80, 256 columns 89 instead of 77; one of 8192, 1024 columns 143 instead of 256;
+// 64 of 2048, 64 columns 190 instead of 115), or where columns leave most of a tile of 128 empty.
 AttendPlan plan_attend(const awe_cache& c, const awe_batch& b, int32_t q_heads) {
+  constexpr int64_t kFewTiles = 900, kTilesPerWide = 3;
   constexpr int64_t kFill = 4096;   // workgroups that keep the chip busy to the end of ragged sequences
   constexpr int64_t kChunk = 1024;  // fewest tokens worth a workgroup of their own
   const int64_t rows = std::min(b.max_rows, b.rows);
   const int64_t cols = rows * (q_heads / c.heads);
+  const int64_t base = (int64_t)b.sequences * c.heads;
+  const int64_t narrow = (cols + 15) / 16, wide = (cols + kRowsColumns - 1) / kRowsColumns;
   AttendPlan p{};
-  p.own_columns = cols > 32;
+  p.own_columns = base * narrow > std::max(kFewTiles, kTilesPerWide * base * wide);
   p.splits = 1;
   if (p.own_columns) {
-    p.groups = (int32_t)((cols + kRowsColumns - 1) / kRowsColumns);
+    p.groups = (int32_t)wide;
     return p;
   }
-  p.groups = (int32_t)((cols + 15) / 16);
-  const int64_t base = (int64_t)b.sequences * c.heads * p.groups;
+  p.groups = (int32_t)narrow;
   const int64_t most = std::max<int64_t>(1, (b.max_length + kChunk - 1) / kChunk);
-  const int64_t want = std::min(most, std::max<int64_t>(1, (kFill + base - 1) / std::max<int64_t>(base, 1)));
+  const int64_t want = std::min(most, std::max<int64_t>(1, (kFill + base * narrow - 1) / std::max<int64_t>(base * narrow, 1)));
   const int64_t chunk = ((b.max_length + want - 1) / want + 255) / 256 * 256;
   p.chunk = (int32_t)std::max<int64_t>(chunk, 256);
   p.splits = (int32_t)std::max<int64_t>(1, (b.max_length + p.chunk - 1) / p.chunk);

@@ -178,14 +178,26 @@ def test_store_bad_tables_and_bounds():
 
 
 # ---- attention ----------------------------------------------------------------------------------
-def run_attend(held, table, counts, lengths, share, t, causal, seed=0, scale=None, size=1.0, **bounds):
+# rows of the tensors, most of which belong to no sequence: with so many, each wave has columns of its own;
+# with the sequences' alone, the tokens are split over the waves
+WIDE = 15360
+
+
+def run_attend(held, table, counts, lengths, share, t, causal, seed=0, scale=None, size=1.0, wide=False, **bounds):
     g = torch.Generator().manual_seed(seed)
-    H = held.heads * share
-    q = (torch.randn(sum(counts), H, held.dim, generator=g) * size).to(T[t])
+    H, n_rows = held.heads * share, sum(counts)
+    q = (torch.randn(n_rows, H, held.dim, generator=g) * size).to(T[t])
     scale = held.dim ** -0.5 if scale is None else scale
+    q_dev = q.cuda()
+    if wide:
+        bounds.update(rows=WIDE, max_rows=WIDE)
+        q_dev = torch.cat([q_dev, torch.full((WIDE - n_rows, H, held.dim), float("nan"), dtype=T[t], device="cuda")])
     b = batch_of(counts, lengths, table, **bounds)
     f = flag()
-    got = awe.attend(upload(held), b, q.cuda(), scale, causal=causal, d_range_flag=f)
+    out = torch.full_like(q_dev, 9.0)
+    awe.attend(upload(held), b, q_dev, scale, causal=causal, out=out, d_range_flag=f)
+    assert bool((out[n_rows:] == 9).all())
+    got = out[:n_rows].clone()
     want, bound = [], []
     at = 0
     for i, (n, length) in enumerate(zip(counts, lengths)):
@@ -195,6 +207,13 @@ def run_attend(held, table, counts, lengths, share, t, causal, seed=0, scale=Non
         at += n
     ref.close(got, np.concatenate(want), np.concatenate(bound), T[t])
     return got, q, f
+
+
+def test_both_ways_are_taken():
+    c = awe.CacheStruct(0, 0, 0, 0, 10, 1, 64, 16)
+    # a workspace is asked for where tokens are split over workgroups, and only there
+    few, many = (awe.BatchStruct(1, 0, 0, 0, 1 << 20, r, r, 60000) for r in (40, WIDE))
+    assert awe.cache_attend_workspace_bytes(c, few, 1) > 0 and awe.cache_attend_workspace_bytes(c, many, 1) == 0
 
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
@@ -208,15 +227,16 @@ def test_attend_single_tokens(share, heads, t, block, dim):
     assert int(f) == 0
 
 
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dim,block,share,t", [(64, 16, 1, "bf16"), (128, 64, 4, "bf16"), (128, 16, 3, "f16"),
-                                               (256, 32, 2, "bf16"), (64, 128, 8, "f16")])
-def test_attend_prompts(dim, block, share, t, causal):
+                                               (256, 32, 2, "bf16"), (64, 128, 8, "f16"), (256, 64, 1, "f16")])
+def test_attend_prompts(dim, block, share, t, causal, wide):
     counts = [1, 7, 64, 0, 130, 33, 5]
     lengths = [1, 7, 100, 40, 130, 300, 3]  # the last: rows before the first token are empty if causal
     nb = sum(-(-n // block) for n in lengths) + 2
     held = ref.Held(nb, 2, dim, block, seed=dim + block)
-    got, _, f = run_attend(held, tables(lengths, block, nb, 4), counts, lengths, share, t, causal)
+    got, _, f = run_attend(held, tables(lengths, block, nb, 4), counts, lengths, share, t, causal, wide=wide)
     if causal:
         assert bool((got[-5:-3] == 0).all()) and bool((got[-3:] != 0).any())
     assert int(f) == 0
@@ -234,8 +254,8 @@ def test_attend_long_sequences_split(share, new):
                max_length=60000)
 
 
-@pytest.mark.parametrize("new", [1, 40])
-def test_attend_blocks_of_very_different_scales(new):
+@pytest.mark.parametrize("new,wide", [(1, False), (40, False), (40, True)])
+def test_attend_blocks_of_very_different_scales(new, wide):
     # one block of large values that gets no weight must not cost the others their digits
     lengths, block = [300], 16
     held = ref.Held(25, 1, 64, block, seed=12)
@@ -244,48 +264,62 @@ def test_attend_blocks_of_very_different_scales(new):
     held.ks[table[0][3]] *= 0
     held.vs[table[0][5]] = 0
     held.vs[table[0][7]] *= 1e-6
-    run_attend(held, table, [new], lengths, 2, "f16", True, scale=0.125, size=8.0)
+    run_attend(held, table, [new], lengths, 2, "f16", True, scale=0.125, size=8.0, wide=wide)
 
 
-@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("new,wide", [(1, False), (40, False), (40, True)])
 @pytest.mark.parametrize("t", ["bf16", "f16"])
-def test_attend_extreme_queries(new, t):
+def test_attend_extreme_queries(new, wide, t):
     # scores of thousands (one token takes all the weight), zero, tiny and large queries, scale 0 and negative
     lengths, block = [200, 200], 16
     held = ref.Held(30, 2, 64, block, seed=13)
     table = tables(lengths, block, 30, 7)
     for size, scale in ((1000.0, 1.0), (0.0, 1.0), (1e-6 if t == "f16" else 1e-30, 1.0), (1.0, 0.0), (1.0, -0.25),
                         (6000.0 if t == "f16" else 1e30, 1e-4 if t == "f16" else 1e-31)):
-        run_attend(held, table, [new, new], lengths, 2, t, True, scale=scale, size=size)
+        run_attend(held, table, [new, new], lengths, 2, t, True, scale=scale, size=size, wide=wide)
 
 
-@pytest.mark.parametrize("new", [1, 40])
-def test_attend_non_finite_rows_stay_alone(new):
+@pytest.mark.parametrize("new,wide", [(1, False), (40, False), (40, True)])
+def test_attend_non_finite_rows_stay_alone(new, wide):
     lengths, block = [100, 90], 16
     held = ref.Held(20, 1, 64, block, seed=14)
     table = tables(lengths, block, 20, 8)
-    clean, q, _ = run_attend(held, table, [new, new], lengths, 2, "bf16", True)
+    clean, q, _ = run_attend(held, table, [new, new], lengths, 2, "bf16", True, wide=wide)
     q[0, 1, 3] = float("nan")
     q[new, 0, 0] = float("inf")
-    got = awe.attend(upload(held), batch_of([new, new], lengths, table), q.cuda(), 0.125)
+    more = dict(rows=WIDE, max_rows=WIDE) if wide else {}
+    q_dev = torch.zeros(WIDE if wide else 2 * new, 2, 64, dtype=torch.bfloat16, device="cuda")
+    q_dev[: 2 * new] = q.cuda()
+    got = awe.attend(upload(held), batch_of([new, new], lengths, table, **more), q_dev, 0.125)[: 2 * new]
     assert bool(torch.isnan(got[0, 1]).all()) and not bool(torch.isfinite(got[new, 0]).any())
     got[0, 1], got[new, 0] = clean[0, 1], clean[new, 0]
     assert torch.equal(got, clean)
 
 
-@pytest.mark.parametrize("new", [1, 20])
-def test_attend_bad_blocks_and_bounds(new):
+@pytest.mark.parametrize("new,wide", [(1, False), (20, False), (20, True)])
+def test_attend_bad_blocks_and_bounds(new, wide):
     lengths, block = [100, 64, 40], 16
     held = ref.Held(20, 2, 64, block, seed=15)
     table = tables(lengths, block, 20, 9)
     table[0, 2], table[1, 0], table[2, :] = 20, -1, 1 << 30
-    _, q, f = run_attend(held, table, [new] * 3, lengths, 2, "bf16", False)  # the third has no token left: zeros
+    # the third has no token left: zeros
+    _, q, f = run_attend(held, table, [new] * 3, lengths, 2, "bf16", False, wide=wide)
     assert int(f) != 0
+    f, n = flag(), WIDE if wide else 3 * new
+    q_dev = torch.zeros(n, *q.shape[1:], dtype=q.dtype, device="cuda")
+    q_dev[: 3 * new] = q.cuda()
+    out = torch.full_like(q_dev, 5.0)
+    b = batch_of([new] * 3, lengths, tables(lengths, block, 20, 9), max_length=70, rows=n, max_rows=n)
+    awe.attend(upload(held), b, q_dev, 0.125, out=out, d_range_flag=f)
+    assert int(f) != 0 and bool((out[:new] == 5).all()) and bool((out[new: 3 * new] != 5).any())
+    # and a cache without any block: zeros, and nothing is read
     f = flag()
-    out = torch.full(q.shape, 5.0, dtype=q.dtype, device="cuda")
-    b = batch_of([new] * 3, lengths, tables(lengths, block, 20, 9), max_length=70)
-    awe.attend(upload(held), b, q.cuda(), 0.125, out=out, d_range_flag=f)
-    assert int(f) != 0 and bool((out[:new] == 5).all()) and bool((out[new:] != 5).any())
+    none = awe.CacheStruct(0, 0, 0, 0, 0, held.heads, held.dim, block)
+    b = batch_of([new] * 3, lengths, tables(lengths, block, 20, 9), rows=n, max_rows=n)
+    size = awe.cache_attend_workspace_bytes(none, b, 4)
+    ws = torch.empty(max(size, 1), dtype=torch.uint8, device="cuda")
+    awe.cache_attend(none, b, q_dev, 4 * 64, 64, 4, awe.BF16, 0.125, 1, out, 4 * 64, 64, ws, size, f)
+    assert int(f) != 0 and bool((out[: 3 * new] == 0).all())
 
 
 def test_attend_strides_and_rows_of_no_sequence():
