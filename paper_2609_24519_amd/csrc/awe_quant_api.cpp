@@ -26,8 +26,9 @@ int64_t elem_bytes(awe_dtype t) { return t == AWE_I8 ? 1 : (t == AWE_F32 ? 4 : 2
 bool is_real(awe_dtype t) { return t == AWE_F32 || t == AWE_BF16 || t == AWE_F16; }
 bool aligned(const void* p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
 
-constexpr int64_t kMost = 0x7fffff00LL;        // sizes of a product, tokens and blocks of a cache
-constexpr int64_t kMostRows = int64_t(1) << 27;  // rows of a batch (they span the grid)
+constexpr int64_t kMost = 0x7fffff00LL;          // sizes of a product, blocks of a cache
+constexpr int64_t kMostTokens = int64_t(1) << 30;  // of a sequence (positions past its end stay within 32 bits)
+constexpr int64_t kMostRows = int64_t(1) << 27;    // of a batch (they span the grid)
 constexpr int64_t kMostStride = int64_t(1) << 40;
 // Bytes from one row of a product's operand to the next: the kernels reach a tile's 256 rows by 32 bits.
 constexpr int64_t kMostRow = int64_t(1) << 24;
@@ -73,7 +74,7 @@ awe_status check_batch(const awe_cache& c, const awe_batch* b) {
   if (b == nullptr) return invalid("batch is NULL");
   if (b->sequences < 0 || b->rows < 0 || b->max_rows < 0 || b->max_length < 0 || b->ld_blocks < 0)
     return invalid("negative size");
-  if (b->rows > kMostRows || b->max_rows > kMostRows || b->max_length > kMost || b->sequences > 0xffffff)
+  if (b->rows > kMostRows || b->max_rows > kMostRows || b->max_length > kMostTokens || b->sequences > 0xffffff)
     return refuse(AWE_ERR_UNSUPPORTED, "too many rows, tokens or sequences");
   if (b->ld_blocks < (b->max_length + c.block - 1) / c.block) return invalid("ld_blocks * block < max_length");
   return AWE_OK;

@@ -648,10 +648,16 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
     }
 }
 
+awe_status too_many() {
+  set_error("too many outputs for one launch");
+  return AWE_ERR_UNSUPPORTED;
+}
+
 template <awe_dtype T, int kFold, int kM, int kN, int kD>
 awe_status launch_rows(const W4Args& a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.g.N + 16 * kN - 1) / (16 * kN)), (unsigned)((a.g.M + 16 * kM - 1) / (16 * kM)));
   const dim3 block(64 * kW);
+  if ((int64_t)grid.x * block.x >= int64_t(1) << 32) return too_many();
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
   if (a.g.s_type == AWE_F32)
     launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F32>);
@@ -669,6 +675,7 @@ awe_status launch_tile(const W4Args& a, int64_t tiles, hipStream_t stream) {
   constexpr int bytes = tile_lds_bytes<T, kM, kN, kG, kFold>();
   static_assert(kG <= 2 && bytes <= 160 * 1024 / (3 - kG), "the workgroups of a CU fit its LDS");
   auto kernel = w4_tile_kernel<T, kM, kN, kG, kFold>;
+  if ((tiles + 7) / 8 * 8 * 256 * kG >= int64_t(1) << 32) return too_many();
   const awe_status st = set_lds_limit(reinterpret_cast<const void*>(kernel), bytes, mu, done);
   if (st != AWE_OK) return st;
   hipLaunchKernelGGL(kernel, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256 * kG), bytes, stream, a);
@@ -678,10 +685,6 @@ awe_status launch_tile(const W4Args& a, int64_t tiles, hipStream_t stream) {
 template <awe_dtype T, int kFold>
 awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
   auto tiles = [&](int cols) { return ((a.g.M + 63) / 64) * ((a.g.N + cols - 1) / cols); };
-  if (tiles(64) > 0xffffff) {
-    set_error("too many tiles");
-    return AWE_ERR_UNSUPPORTED;
-  }
   // the widest tile that still gives each of the 256 CUs one; two workgroups per CU where there are enough
   if constexpr (kFold > 1) {  // (a fold at every step needs more registers than such a tile leaves)
     if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFold>(a, tiles(256), stream);

@@ -64,6 +64,16 @@ def test_exact_sums(M, N, K, group, x, zeros):
     assert np.abs(want).max() * 4 < 2 ** 22 and np.array_equal(ref.f64(got), want)
 
 
+@pytest.mark.parametrize("x,zeros", [("bf16", True), ("f16", False), ("i8", True)])
+@pytest.mark.parametrize("M,N,K,group", [(3, 4200, 300, 64), (16, 5000, 1100, 128), (40, 4200, 260, 32), (40, 4100, 520, 128),
+                                         (65, 16400, 130, 32), (65, 16400, 300, 64), (70, 32900, 300, 128),
+                                         (65, 32800, 450, 64), (65, 65600, 257, 128), (66, 65600, 384, 64)])
+def test_many_outputs(M, N, K, group, x, zeros):
+    # sizes at which workgroups have 32, 128 and 256 outputs, one or two of them per CU
+    d = inputs(M, N, K, group, x, "bf16", zeros, seed=N)
+    check(d, group, "f32")
+
+
 @pytest.mark.parametrize("M", [1, 2, 16, 20, 50, 100, 300])
 @pytest.mark.parametrize("x", ["bf16", "i8"])
 def test_strides_and_alignment(M, x):
