@@ -291,22 +291,21 @@ awe_status awe_gemm_crt(int64_t M, int64_t N, int64_t K, const int64_t* A, int64
    Products with 4-bit weights that carry a scale per group, and attention over keys and values
    held in 8 bits.  Integers are multiplied as integers or as floating-point numbers that hold them
    exactly; sums, scales and softmax statistics are FP32, and each result is rounded once to its
-   type (nearest, ties to even).  Results are the same on every run and the same for every row
-   whatever else the call holds, except that they depend on which kernel the sizes select.
-   The calls enqueue only kernels, allocate nothing, keep nothing and need no first call: they
-   can be captured into a graph at any time, and overlap on any streams as long as no call
-   writes what another uses.  Outputs share no memory with inputs or a workspace. */
+   type (nearest, ties to even).  Results are the same on every run and do not depend on a call's
+   other rows, except that the sizes select the kernel and with it the order of sums.  The calls
+   enqueue only kernels, allocate nothing and keep nothing: they can be captured into a graph at
+   any time, and overlap on any streams as long as no call writes what another uses.  Outputs share no memory with inputs or a workspace. */
 
 /* Y = X W^T with 4-bit weights: for i < M, j < N
      Y[i,j] = x_scales[i] * sum_g w_scales[j,g] * sum_{k in group g} X[i,k] * (u[j,k] - z[j,g]).
    X is M x K (x_type AWE_BF16, AWE_F16 or AWE_I8, leading dimension ldx).  Row j of W holds the
    codes u[j,k] in 0..15 of output j: byte W[j*ldw + k/2], the low nibble for even k, ldw >=
-   ceil(K/2) bytes (at an odd K the last high nibble is ignored).  Group g covers indices
+   ceil(K/2) bytes (at an odd K the last high nibble is ignored; rows at odd addresses take longer).  Group g covers indices
    g*group .. g*group + group - 1; group is a multiple of 32, or at least K (one group); the last
    group may be short.  w_scales[j*lds + g] has s_type (AWE_F32, AWE_BF16, AWE_F16), zero points
    zeros[j*ldz + g] are bytes, and NULL stands for 8 everywhere (codes of -8..7).  x_scales: FP32, for
    AWE_I8 only, NULL for 1.  Y is M x N of y_type (AWE_F32, AWE_BF16, AWE_F16).  Pointers are aligned to
-   their element; rows may begin anywhere.  K = 0 writes zeros.  A NaN or infinity in a row of X
+   their element; rows may begin anywhere, less than 16 MiB apart.  K = 0 writes zeros.  A NaN or infinity in a row of X
    reaches that row of Y alone. */
 awe_status awe_gemm_w4(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, awe_dtype x_type,
                        const float* x_scales, const uint8_t* W, int64_t ldw, const void* w_scales, int64_t lds,
@@ -356,7 +355,7 @@ typedef struct awe_batch {
    in FP32, within [-127, 127], and q = 0 where s' = 0.  The scale of a block never shrinks while
    tokens are added to it.  A NaN or infinity is stored as 0 and sets *d_range_flag.  Bytes of a
    block past the sequence's length keep their contents.  A block that a call writes must
-   belong to one sequence of the call only (else that block's contents are unspecified). */
+   belong to one entry of one sequence's table only (else that block's contents are unspecified). */
 awe_status awe_cache_store(const awe_cache* cache, const awe_batch* batch, const void* k, int64_t k_row,
                            int64_t k_head, const void* v, int64_t v_row, int64_t v_head, awe_dtype type,
                            int32_t* d_range_flag, hipStream_t stream);
@@ -374,7 +373,8 @@ awe_status awe_cache_load(const awe_cache* cache, const awe_batch* batch, void* 
      out = softmax_j(scale * q . k_j) v_j  over tokens j < lengths[b], and for causal != 0 up to the row's
    own position only.  A row without any token gets zeros.  max_length also sets how the tokens are
    split over workgroups: a bound near the longest length is best.  The weights of the second
-   product are rounded to FP16 (two FP16 numbers each for AWE_F16).  The workspace
+   product are rounded to FP16 (two FP16 numbers each for AWE_F16).  Scores past FP32's range give
+   no number.  The workspace
    (awe_cache_attend_workspace_bytes, aligned to 16 bytes; 0 bytes for most prompts) holds the parts
    of split sequences until the call's kernels have run. */
 awe_status awe_cache_attend_workspace_bytes(const awe_cache* cache, const awe_batch* batch, int32_t q_heads,

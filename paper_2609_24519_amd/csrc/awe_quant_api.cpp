@@ -50,7 +50,7 @@ awe_status w4_impl(const W4Launch& g, hipStream_t stream) {
     if (g.x == nullptr || g.w == nullptr || g.scales == nullptr) return invalid("X, W or w_scales is NULL");
     if (g.ldx < g.K || g.ldw < (g.K + 1) / 2 || g.lds < groups || (g.zeros != nullptr && g.ldz < groups))
       return invalid("leading dimension too small");
-    if (g.ldx * elem_bytes(g.x_type) >= kMostRow || g.ldw >= kMostRow || g.lds * elem_bytes(g.s_type) >= kMostRow ||
+    if (g.ldx >= kMostRow / elem_bytes(g.x_type) || g.ldw >= kMostRow || g.lds >= kMostRow / elem_bytes(g.s_type) ||
         (g.zeros != nullptr && g.ldz >= kMostRow))
       return refuse(AWE_ERR_UNSUPPORTED, "rows of an operand too far apart");
     if (!aligned(g.x, elem_bytes(g.x_type)) || !aligned(g.scales, elem_bytes(g.s_type)) || !aligned(g.x_scales, 4))
@@ -107,8 +107,9 @@ awe_status check_rows(const Rows& r, awe_dtype type) {
 
 // Whether the elements of a written row tensor are distinct: heads inside rows, or rows inside heads.
 bool distinct(const Rows& r, int64_t rows, int64_t heads, int64_t dim) {
-  const bool by_row = (heads == 1 || r.head >= dim) && (rows == 1 || r.row >= (heads - 1) * r.head + dim);
-  const bool by_head = (rows == 1 || r.row >= dim) && (heads == 1 || r.head >= (rows - 1) * r.row + dim);
+  using Wide = __int128;  // kMostRows rows at a stride of kMostStride pass 64 bits
+  const bool by_row = (heads == 1 || r.head >= dim) && (rows == 1 || r.row >= Wide(heads - 1) * r.head + dim);
+  const bool by_head = (rows == 1 || r.row >= dim) && (heads == 1 || r.head >= Wide(rows - 1) * r.row + dim);
   return by_row || by_head;
 }
 
@@ -150,7 +151,8 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
   if (st == AWE_OK) st = check_rows(o, type);
   if (st != AWE_OK) return st;
   if (!distinct(o, batch->rows, q_heads, cache->head_dim)) return invalid("written elements share memory");
-  if (std::min(batch->rows, batch->max_rows) * q_heads > (int64_t(1) << 30)) return refuse(AWE_ERR_UNSUPPORTED, "too many rows");
+  if (std::min(batch->rows, batch->max_rows) * q_heads > (int64_t(1) << 30))
+    return refuse(AWE_ERR_UNSUPPORTED, "too many rows");
   const size_t need = plan_attend(*cache, *batch, q_heads).workspace;
   if (need > 0 && (ws == nullptr || ws_bytes < need))
     return refuse(AWE_ERR_WORKSPACE, "workspace smaller than awe_cache_attend_workspace_bytes");

@@ -32,6 +32,11 @@ def test_w4_sizes():
     assert w4(M=0, X=None, Y=None) == awe.OK and w4(N=0, W=None, Y=None) == awe.OK
     assert w4(M=1 << 31) == awe.ERR_UNSUPPORTED and w4(N=1 << 31, ldy=1 << 31) == awe.ERR_UNSUPPORTED
     assert w4(K=1 << 31, ldx=1 << 31) == awe.ERR_UNSUPPORTED
+    # rows 16 MiB apart and more, up to strides whose bytes pass 64 bits
+    for far in (1 << 24, 1 << 62):
+        assert w4(ldx=far // 2) == awe.ERR_UNSUPPORTED and w4(ldw=far) == awe.ERR_UNSUPPORTED
+        assert w4(lds=far // 4) == awe.ERR_UNSUPPORTED and w4(zeros=P, ldz=far) == awe.ERR_UNSUPPORTED
+    assert w4(ldx=1 << 62) == awe.ERR_UNSUPPORTED and w4(lds=1 << 62) == awe.ERR_UNSUPPORTED
 
 
 def cache(**kw):
@@ -75,7 +80,7 @@ def test_cache_and_batch_refusals(call):
                 dict(ld_blocks=3), dict(starts=None), dict(lengths=None), dict(blocks=None), dict(starts=P + 2),
                 dict(lengths=P + 1), dict(blocks=P + 2)):
         assert call(b=batch(**bad)) == awe.ERR_INVALID_VALUE, bad
-    for bad in (dict(rows=1 << 28), dict(max_rows=1 << 28), dict(max_length=1 << 31, ld_blocks=1 << 31),
+    for bad in (dict(rows=1 << 28), dict(max_rows=1 << 28), dict(max_length=(1 << 30) + 1, ld_blocks=1 << 31),
                 dict(sequences=1 << 24)):
         assert call(b=batch(**bad)) == awe.ERR_UNSUPPORTED, bad
     for nothing in (dict(sequences=0), dict(rows=0), dict(max_rows=0)):
@@ -95,6 +100,9 @@ def test_row_refusals(load):
     if load:  # written elements that share memory
         for bad in (dict(k_row=0), dict(k_row=127), dict(v_head=63), dict(v_row=64, v_head=64)):
             assert tokens(load, **bad) == awe.ERR_INVALID_VALUE, bad
+        # rows * stride past 64 bits
+        far = dict(k_row=1 << 40, k_head=1 << 39)
+        assert tokens(load, b=batch(rows=(1 << 23) + 1, max_rows=1), c=cache(heads=3), **far) == awe.ERR_INVALID_VALUE
 
 
 def test_attend_refusals():
@@ -149,5 +157,9 @@ def test_conveniences_check_shapes():
         awe.attend(c, b, q[:4], 1.0)
     with pytest.raises(ValueError):
         awe.attend(c, b, q.float(), 1.0)
+    for call in (lambda: awe.matmul_w4(h, w, s, 32), lambda: awe.store_tokens(c, b, q, q),
+                 lambda: awe.attend(c, b, q, 1.0)):  # tensors of the host
+        with pytest.raises(ValueError):
+            call()
     with pytest.raises(ValueError):  # past the entries of the table
         awe.attend(c, awe.Batch(i32(3), i32(2), i32(2, 3), 5, 3, 64), q, 1.0)
