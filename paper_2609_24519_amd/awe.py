@@ -405,7 +405,7 @@ def _rows_2d(t, what):
     (rows, cols), (ld, one) = t.shape, t.stride()
     if (one != 1 and cols > 1) or (ld < cols and rows > 1):
         raise ValueError("%s must have adjacent elements in its rows, and rows that share no memory" % what)
-    return ld if ld > cols else cols
+    return ld if ld > cols and rows > 1 else cols
 
 
 def matmul_w4(x, w, scales, group, zeros=None, x_scales=None, out_dtype=None):
@@ -458,9 +458,10 @@ class Cache:
         for s in (k_scales, v_scales):
             if s.shape != (blocks, heads) or _dtype(s.dtype, _FLOAT32) != F32:
                 raise ValueError("scales must be float32 of blocks x heads")
+        at = k.device
         for t in (k, v, k_scales, v_scales):
-            if not t.is_contiguous():
-                raise ValueError("the cache's tensors must be contiguous")
+            if not t.is_contiguous() or t.device != at:
+                raise ValueError("the cache's tensors must be contiguous, and on one device")
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
         self.heads, self.head_dim, self.block = heads, dim, block
         self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), blocks,
@@ -488,6 +489,8 @@ class Batch:
             raise ValueError("starts, lengths and blocks must have sequences + 1, sequences and sequences rows")
         if not starts.is_contiguous() or not lengths.is_contiguous():
             raise ValueError("starts and lengths must be contiguous")
+        if lengths.device != starts.device or blocks.device != starts.device:
+            raise ValueError("starts, lengths and blocks must be on one device")
         ld = _rows_2d(blocks, "blocks")
         self.starts, self.lengths, self.blocks, self.rows = starts, lengths, blocks, rows
         # the last row holds blocks.shape[1] entries, so no position may lie past them
@@ -510,6 +513,12 @@ def _fits(cache, batch):
         raise ValueError("max_length lies past the block table's entries")
 
 
+def _flag(t):
+    if t is not None:
+        _dtype(t.dtype, _INT32)
+    return t
+
+
 def store_tokens(cache, batch, k, v, d_range_flag=None):
     """Stores k and v (rows x heads x dim) as the newest tokens of the batch's sequences."""
     _fits(cache, batch)
@@ -517,7 +526,7 @@ def store_tokens(cache, batch, k, v, d_range_flag=None):
     v_row, v_head = _row_tensor(v, cache, batch, cache.heads, "v")
     if k.dtype != v.dtype:
         raise ValueError("k and v have different types")
-    _on_current_device(cache.k, batch.starts, k, v)
+    _on_current_device(cache.k, batch.starts, k, v, _flag(d_range_flag))
     cache_store(cache, batch, k, k_row, k_head, v, v_row, v_head, _dtype(k.dtype, (F32, BF16, F16)), d_range_flag)
 
 
@@ -526,7 +535,7 @@ def load_tokens(cache, batch, dtype, d_range_flag=None):
     Rows that belong to no sequence are not written."""
     import torch
     _fits(cache, batch)
-    _on_current_device(cache.k, batch.starts)
+    _on_current_device(cache.k, batch.starts, _flag(d_range_flag))
     shape = (batch.rows, cache.heads, cache.head_dim)
     k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
     row, head = shape[1] * shape[2], shape[2]
@@ -546,7 +555,7 @@ def attend(cache, batch, q, scale, causal=True, out=None, d_range_flag=None):
     elif out.dtype != q.dtype:
         raise ValueError("out and q have different types")
     out_row, out_head = _row_tensor(out, cache, batch, heads, "out")
-    _on_current_device(cache.k, batch.starts, q, out)
+    _on_current_device(cache.k, batch.starts, q, out, _flag(d_range_flag))
     n = cache_attend_workspace_bytes(cache, batch, heads)
     ws = q.new_empty(n, dtype=_torch.uint8) if n else None
     cache_attend(cache, batch, q, q_row, q_head, heads, dtype, scale, 1 if causal else 0, out, out_row, out_head, ws,

@@ -56,7 +56,9 @@ awe_status w4_impl(const W4Launch& g, hipStream_t stream) {
     if (!aligned(g.x, elem_bytes(g.x_type)) || !aligned(g.scales, elem_bytes(g.s_type)) || !aligned(g.x_scales, 4))
       return invalid("an operand is not aligned to its element");
   }
-  return launch_w4(g, stream);
+  W4Launch h = g;
+  if (h.K == 0) h.x_scales = nullptr;  // zeros, whatever the scales are
+  return launch_w4(h, stream);
 }
 
 awe_status check_cache(const awe_cache* c) {

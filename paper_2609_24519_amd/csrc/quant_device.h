@@ -16,11 +16,6 @@ namespace {
 using bf16 = __bf16;
 using f16 = _Float16;
 
-__device__ __forceinline__ float load_real(const void* p, int64_t i, awe_dtype t) {
-  if (t == AWE_F32) return reinterpret_cast<const float*>(p)[i];
-  if (t == AWE_BF16) return (float)reinterpret_cast<const bf16*>(p)[i];
-  return (float)reinterpret_cast<const f16*>(p)[i];
-}
 // Rounds to nearest, ties to even.
 __device__ __forceinline__ void store_real(void* p, int64_t i, awe_dtype t, float v) {
   if (t == AWE_F32)

@@ -104,6 +104,9 @@ def test_empty_reduction_writes_zeros():
         x, w = torch.zeros(M, 0, dtype=torch.bfloat16, device="cuda"), torch.zeros(9, 0, dtype=torch.uint8, device="cuda")
         y = awe.matmul_w4(x, w, torch.zeros(9, 0, device="cuda"), 32)
         assert y.shape == (M, 9) and bool((y == 0).all())
+    d_scales = torch.full((70,), float("inf"), device="cuda")
+    y = awe.matmul_w4(x.to(torch.int8), w, torch.zeros(9, 0, device="cuda"), 32, x_scales=d_scales)
+    assert bool((y == 0).all())
     assert awe.matmul_w4(x[:0], w, torch.zeros(9, 0, device="cuda"), 32).shape == (0, 9)
 
 
@@ -118,6 +121,17 @@ def test_nan_and_infinity_stay_in_their_row(M):
     assert bool(torch.isnan(y[1]).all()) and not bool(torch.isfinite(y[2]).any())
     keep = [i for i in range(M) if i not in (1, 2)]
     assert torch.equal(y[keep], clean[keep])
+
+
+@pytest.mark.parametrize("x,power", [("bf16", -130), ("f16", -20)])
+@pytest.mark.parametrize("M", [3, 40, 100])
+def test_subnormal_rows(M, x, power):
+    # elements below the type's smallest normal number count in full
+    N, K, group = 80, 512, 128
+    d = inputs(M, N, K, group, x, "f32", True, seed=4)
+    d["x"][:] = (d["x"].float() * 2.0 ** power).to(T[x])
+    d["scales"] *= 2.0 ** 60
+    check(d, group, "f32")
 
 
 def test_scales_of_zero_and_far_apart():

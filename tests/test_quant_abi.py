@@ -157,6 +157,14 @@ def test_conveniences_check_shapes():
         awe.attend(c, b, q[:4], 1.0)
     with pytest.raises(ValueError):
         awe.attend(c, b, q.float(), 1.0)
+    for flag in (torch.zeros(1), torch.zeros(1, dtype=torch.int64)):
+        with pytest.raises(ValueError):
+            awe.attend(c, b, q, 1.0, d_range_flag=flag)
+    far = [torch.zeros(s, dtype=t, device="meta") for s, t in (((4, 2), torch.float32), ((2,), torch.int32))]
+    with pytest.raises(ValueError):  # tensors of two devices
+        awe.Cache(i8(4, 2, 16, 64), i8(4, 2, 64, 16), f, far[0])
+    with pytest.raises(ValueError):
+        awe.Batch(i32(3), far[1], i32(2, 4), 5, 3, 64)
     for call in (lambda: awe.matmul_w4(h, w, s, 32), lambda: awe.store_tokens(c, b, q, q),
                  lambda: awe.attend(c, b, q, 1.0)):  # tensors of the host
         with pytest.raises(ValueError):
