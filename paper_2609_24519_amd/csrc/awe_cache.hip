@@ -7,8 +7,12 @@ namespace {
 
 // ---- store and load -------------------------------------------------------------------------
 // One workgroup per touched block, head and tensor: workgroup (j, head, tensor + 2 * sequence) takes the
-// sequence's j-th block that gets rows.  Bound by the rows' and the cache's bytes: rows are moved
-// eight elements a thread; values, which are kept by dimension, are turned over in LDS.
+// sequence's j-th block that gets rows.  Bound by the rows' and the cache's bytes, and by the chain of reads that
+// leads to them (starts and lengths, table, rows, then the largest); for 5100 rows of 8 heads of 128 in
+// BF16, storing takes 12 us (31 MB, 2.6 TB/s), loading 8 (31 MB, 3.9 TB/s).  A thread has up to kPatches
+// patches of four adjacent tokens by eight dimensions; storing keeps them in registers between the search for
+// the largest and the rounding, so rows are read once (reading them twice, and dividing by the scale: 18.6 us).  Values, which are kept by dimension, are turned over in
+// LDS, a word of four tokens at a time.
 struct Tile {
   int32_t id, t0, t1;  // block (-1: nothing to do), slots that get rows
   int64_t row0;        // row of slot 0 (of slot t0 at the earliest)
@@ -22,60 +26,143 @@ __device__ __forceinline__ Tile tile_of(const CacheLaunch& g) {
   return Tile{id, pos0 > first ? pos0 - first : 0, std::min(s.len - first, g.c.block), (int64_t)s.row0 + first - pos0};
 }
 
-// Eight elements of a row from any address, as floats.
+// Eight elements of a row at any address, as words and as floats.
 template <class E>
 struct __attribute__((packed)) Any8Of {
   E v[8];
 };
-constexpr float kLargest = 3.402823466e38f;
+template <class E>
+struct __attribute__((packed)) Words {
+  static constexpr int kN = 2 * sizeof(E);
+  uint32_t w[kN];
 
-__device__ __forceinline__ int8_t quantised(float x, float scale) {
-  return scale > 0.f && fabsf(x) <= kLargest ? (int8_t)fminf(fmaxf(rintf(x / scale), -127.f), 127.f) : (int8_t)0;
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (std::is_same<E, float>::value) return __builtin_bit_cast(float, w[i]);
+    if constexpr (std::is_same<E, bf16>::value) return __builtin_bit_cast(float, i % 2 == 0 ? w[i / 2] << 16 : w[i / 2] & 0xffff0000u);
+    return (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i / 2] >> (16 * (i % 2))));
+  }
+};
+// The largest magnitudes of words of elements, as bits: whole numbers are ordered as the magnitudes are, and an
+// infinity or a NaN is at least kBad.
+template <class E>
+struct Magnitude {
+  typedef uint16_t u2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kBad = std::is_same<E, float>::value ? 0x7f800000u : std::is_same<E, bf16>::value ? 0x7f80u : 0x7c00u;
+  static __device__ __forceinline__ uint32_t larger(uint32_t most, uint32_t w) {
+    if constexpr (sizeof(E) == 4) return std::max(most, w & 0x7fffffffu);
+    const uint32_t m = w & 0x7fff7fffu;
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u2, most), __builtin_bit_cast(u2, m)));
+  }
+  static __device__ __forceinline__ uint32_t top(uint32_t most) {  // of a word's elements
+    return sizeof(E) == 4 ? most : std::max(most & 0xffffu, most >> 16);
+  }
+  static __device__ __forceinline__ uint32_t finite(uint32_t w) {  // 0 for the elements that are not
+    if constexpr (sizeof(E) == 4) return (w & 0x7fffffffu) >= kBad ? 0u : w;
+    return ((w & 0x7fffu) >= kBad ? 0u : w & 0xffffu) | (((w >> 16) & 0x7fffu) >= kBad ? 0u : w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ float value(uint32_t top) {
+    return Words<E>{{sizeof(E) == 4 ? top : top & 0xffffu}}.value(0);
+  }
+};
+
+// rint(x / scale) within [-127, 127], its low byte the result's, for finite x and one scale > 0.  With
+// both brought to a scale in [1, 2) (exactly, but for x far below half a step), q = x y for the rounded reciprocal
+// y of the scale is within an ulp of the quotient, and one step with the exact remainder rounds it correctly; so this
+// is the quotient of the formula in 3 instructions, not the 10 of a division.  Adding 1.5 2^23 rounds to
+// a whole number, ties to even.
+struct Quantiser {
+  float unit, reciprocal;
+  int power;
+  __device__ __forceinline__ explicit Quantiser(float scale)
+      : power(scale > 0.f ? 1 - __builtin_amdgcn_frexp_expf(scale) : 0) {
+    unit = scale > 0.f ? ldexpf(scale, power) : 1.f;
+    reciprocal = 1.f / unit;
+  }
+  __device__ __forceinline__ uint32_t operator()(float x) const {
+    x = __builtin_amdgcn_ldexpf(x, power);
+    float q = x * reciprocal;
+    q = __builtin_fmaf(__builtin_fmaf(-q, unit, x), reciprocal, q);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_fmed3f(q, -127.f, 127.f) + 12582912.f);
+  }
+};
+// The low bytes of four words.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
 // Dynamic LDS: a block of values by dimension, rows padded by a word.
 extern __shared__ uint8_t turned[];
 size_t turned_bytes(const awe_cache& c) { return (size_t)c.head_dim * (c.block + 4); }
 
-template <class E>
+// The patches of a block: the e-th covers slots slot .. slot + 3 (some of which may get no row) and
+// dimensions d .. d + 7.
+struct Patch {
+  int32_t slot, d;
+};
+__device__ __forceinline__ int patches(const Tile& t, int D) { return ((t.t1 + 3) / 4 - t.t0 / 4) * (D / 8); }
+__device__ __forceinline__ Patch patch(const Tile& t, int D, int e) {
+  return Patch{4 * (t.t0 / 4 + e / (D / 8)), 8 * (e % (D / 8))};
+}
+
+template <class E, int kPatches>
 __global__ __launch_bounds__(256) void store_kernel(CacheLaunch g) {
   const Tile t = tile_of(g);
   if (t.id < 0) return;
   const bool values = blockIdx.z & 1;
-  const int head = blockIdx.y, D = g.c.head_dim, block = g.c.block, per_row = D / 8;
+  const int head = blockIdx.y, D = g.c.head_dim, block = g.c.block, threads = blockDim.x;
   const Rows& r = values ? g.v : g.k;
   const int64_t at = (int64_t)t.id * g.c.heads + head;
   int8_t* q = (values ? g.c.v : g.c.k) + at * block * D;
   float* scale = (values ? g.c.v_scales : g.c.k_scales) + at;
   const E* rows = reinterpret_cast<const E*>(r.p) + t.row0 * r.row + head * r.head;
-  auto piece = [&](int e) {  // the e-th eight elements
-    return *reinterpret_cast<const Any8Of<E>*>(rows + (t.t0 + e / per_row) * r.row + 8 * (e % per_row));
-  };
-  const int pieces = (t.t1 - t.t0) * per_row;
-  float most = 0.f;
-  bool bad = false;
-  for (int e = threadIdx.x; e < pieces; e += 256) {
-    const Any8Of<E> v = piece(e);
+  const int n = patches(t, D);
+  Words<E> x[kPatches][4] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float x = fabsf((float)v.v[i]);
-      bad |= !(x <= kLargest);
-      most = x <= kLargest ? fmaxf(most, x) : most;
-    }
+  for (int u = 0; u < kPatches; ++u) {
+    const int e = threadIdx.x + u * threads;
+    if (e >= n) break;
+    const Patch at = patch(t, D, e);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (at.slot + k >= t.t0 && at.slot + k < t.t1)
+        x[u][k] = *reinterpret_cast<const Words<E>*>(rows + (at.slot + k) * r.row + at.d);
   }
-  if (bad && g.flag != nullptr) *g.flag = 1;
+  const float old = t.t0 > 0 ? *scale : 0.f;
+  using Size = Magnitude<E>;
+  auto largest = [&] {
+    uint32_t m = 0;
+#pragma unroll
+    for (int u = 0; u < kPatches; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int w = 0; w < Words<E>::kN; ++w) m = Size::larger(m, x[u][k].w[w]);
+    return Size::top(m);
+  };
+  uint32_t top = largest();
+  if (top >= Size::kBad) {
+    if (g.flag != nullptr) *g.flag = 1;
+#pragma unroll
+    for (int u = 0; u < kPatches; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int w = 0; w < Words<E>::kN; ++w) x[u][k].w[w] = Size::finite(x[u][k].w[w]);
+    top = largest();
+  }
+  float most = Size::value(top);
   __shared__ float part[4];
   for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
-  const float old = t.t0 > 0 ? *scale : 0.f;
   __syncthreads();  // (every thread has read the old scale)
-  const float now = fmaxf(old, fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) / 127.f);
+  for (int w = 0; w < threads / 64; ++w) most = fmaxf(most, part[w]);
+  const float now = fmaxf(old, most / 127.f);
   if (threadIdx.x == 0) *scale = now;
   if (now != old && t.t0 > 0) {
     // the older tokens on the new scale, 16 bytes at a time: keys' first t0 rows, values' first t0 columns
     const float ratio = old / now;
     const int chunks = values ? (t.t0 + 15) / 16 : D / 16, lines = values ? D : t.t0, line = values ? block : D;
-    for (int e = threadIdx.x; e < lines * chunks; e += 256) {
+    for (int e = threadIdx.x; e < lines * chunks; e += threads) {
       const int c = e % chunks;
       uint4* p = reinterpret_cast<uint4*>(q + (e / chunks) * line + 16 * c);
       const int keep = values ? t.t0 - 16 * c : 16;  // the bytes after these are not older tokens
@@ -89,50 +176,59 @@ __global__ __launch_bounds__(256) void store_kernel(CacheLaunch g) {
     __syncthreads();  // the rows' bytes share words with these
   }
   const int stride = block + 4;
-  for (int e = threadIdx.x; e < pieces; e += 256) {
-    const Any8Of<E> v = piece(e);
-    const int slot = t.t0 + e / per_row, d = 8 * (e % per_row);
-    union {
-      int8_t b[8];
-      uint2 w;
-    } o;
+  const Quantiser byte_of(now);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.b[i] = quantised((float)v.v[i], now);
+  for (int u = 0; u < kPatches; ++u) {
+    const int e = threadIdx.x + u * threads;
+    if (e >= n) break;
+    const Patch at = patch(t, D, e);
+    uint32_t b[4][8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[k][i] = now > 0.f ? byte_of(x[u][k].value(i)) : 0u;
     if (!values) {
-      *reinterpret_cast<uint2*>(q + slot * D + d) = o.w;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (at.slot + k >= t.t0 && at.slot + k < t.t1)
+          *reinterpret_cast<uint2*>(q + (at.slot + k) * D + at.d) =
+              uint2{low_bytes(b[k][0], b[k][1], b[k][2], b[k][3]), low_bytes(b[k][4], b[k][5], b[k][6], b[k][7])};
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) turned[(d + i) * stride + slot] = (uint8_t)o.b[i];
+      for (int i = 0; i < 8; ++i)
+        *reinterpret_cast<uint32_t*>(turned + (at.d + i) * stride + at.slot) = low_bytes(b[0][i], b[1][i], b[2][i], b[3][i]);
     }
   }
   if (!values) return;
   __syncthreads();
   if (t.t0 == 0 && t.t1 == block) {
-    for (int e = threadIdx.x; e < D * block / 16; e += 256) {
+    for (int e = threadIdx.x; e < D * block / 16; e += threads) {
       const int d = e / (block / 16), c = e % (block / 16);
       const uint32_t* w = reinterpret_cast<const uint32_t*>(turned + d * stride + 16 * c);
       reinterpret_cast<uint4*>(q)[e] = uint4{w[0], w[1], w[2], w[3]};
     }
   } else {
-    const int n = t.t1 - t.t0;
-    for (int e = threadIdx.x; e < D * n; e += 256) q[e / n * block + t.t0 + e % n] = (int8_t)turned[e / n * stride + t.t0 + e % n];
+    const int len = t.t1 - t.t0;
+    for (int e = threadIdx.x; e < D * len; e += threads)
+      q[e / len * block + t.t0 + e % len] = (int8_t)turned[e / len * stride + t.t0 + e % len];
   }
 }
 
-template <class E>
+template <class E, int kPatches>
 __global__ __launch_bounds__(256) void load_kernel(CacheLaunch g) {
   const Tile t = tile_of(g);
   if (t.id < 0) return;
   const bool values = blockIdx.z & 1;
-  const int head = blockIdx.y, D = g.c.head_dim, block = g.c.block, per_row = D / 8, stride = block + 4;
+  const int head = blockIdx.y, D = g.c.head_dim, block = g.c.block, stride = block + 4, threads = blockDim.x;
   const Rows& r = values ? g.v : g.k;
   const int64_t at = (int64_t)t.id * g.c.heads + head;
   const int8_t* q = (values ? g.c.v : g.c.k) + at * block * D;
   const float scale = (values ? g.c.v_scales : g.c.k_scales)[at];
   E* rows = reinterpret_cast<E*>(r.p) + t.row0 * r.row + head * r.head;
+  const int n = patches(t, D);
   if (values) {
     const int c0 = t.t0 / 16, chunks = (t.t1 + 15) / 16 - c0;  // those that hold the slots
-    for (int e = threadIdx.x; e < D * chunks; e += 256) {
+    for (int e = threadIdx.x; e < D * chunks; e += threads) {
       const int d = e / chunks, c = c0 + e % chunks;
       const uint4 w = *reinterpret_cast<const uint4*>(q + d * block + 16 * c);
       uint32_t* p = reinterpret_cast<uint32_t*>(turned + d * stride + 16 * c);
@@ -140,22 +236,34 @@ __global__ __launch_bounds__(256) void load_kernel(CacheLaunch g) {
     }
     __syncthreads();
   }
-  for (int e = threadIdx.x; e < (t.t1 - t.t0) * per_row; e += 256) {
-    const int slot = t.t0 + e / per_row, d = 8 * (e % per_row);
-    union {
-      int8_t b[8];
-      uint2 w;
-    } o;
-    if (!values) {
-      o.w = *reinterpret_cast<const uint2*>(q + slot * D + d);
-    } else {
+  // the patches' rows, from byte(k, i): dimension i of the k-th token, sign-extended or with bytes above it
+  auto write = [&](const Patch& at, auto byte) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o.b[i] = (int8_t)turned[(d + i) * stride + slot];
+    for (int k = 0; k < 4; ++k) {
+      if (at.slot + k < t.t0 || at.slot + k >= t.t1) continue;
+      Any8Of<E> v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v.v[i] = (E)((float)(int8_t)byte(k, i) * scale);
+      *reinterpret_cast<Any8Of<E>*>(rows + (at.slot + k) * r.row + at.d) = v;
     }
-    Any8Of<E> v;
+  };
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v.v[i] = (E)((float)o.b[i] * scale);
-    *reinterpret_cast<Any8Of<E>*>(rows + slot * r.row + d) = v;
+  for (int u = 0; u < kPatches; ++u) {
+    const int e = threadIdx.x + u * threads;
+    if (e >= n) break;
+    const Patch at = patch(t, D, e);
+    if (values) {
+      uint32_t w[8];  // four tokens each
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const uint32_t*>(turned + (at.d + i) * stride + at.slot);
+      write(at, [&](int k, int i) { return w[i] >> (8 * k); });
+    } else {
+      uint2 w[4];  // (slots without a row: the first one that has a row again)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w[k] = *reinterpret_cast<const uint2*>(q + (at.slot + k >= t.t0 && at.slot + k < t.t1 ? at.slot + k : t.t0) * D + at.d);
+      write(at, [&](int k, int i) { return (i < 4 ? w[k].x : w[k].y) >> (8 * (i % 4)); });
+    }
   }
 }
 
@@ -722,7 +830,7 @@ __global__ __launch_bounds__(64 * kWaves) void attend_join_kernel(AttendArgs a) 
 
 // Grid (blocks that can be touched, heads, 2 * sequences); sequences go over in parts of the grid's limit.
 template <class K>
-awe_status launch_tiles(K kernel, CacheLaunch g, const char* what, hipStream_t stream) {
+awe_status launch_blocks(K kernel, CacheLaunch g, int threads, const char* what, hipStream_t stream) {
   // n rows touch at most 1 + ceil((n - 1) / block) blocks
   const unsigned x = (unsigned)((std::min(g.b.max_rows, g.b.rows) + g.c.block - 2) / g.c.block + 1);
   const int32_t all = g.b.sequences;
@@ -732,28 +840,35 @@ awe_status launch_tiles(K kernel, CacheLaunch g, const char* what, hipStream_t s
     part.b.starts += s;
     part.b.lengths += s;
     part.b.blocks += s * g.b.ld_blocks;
-    hipLaunchKernelGGL(kernel, dim3(x, (unsigned)g.c.heads, 2u * part.b.sequences), dim3(256), turned_bytes(g.c), stream, part);
+    hipLaunchKernelGGL(kernel, dim3(x, (unsigned)g.c.heads, 2u * part.b.sequences), dim3(threads), turned_bytes(g.c), stream, part);
     const awe_status st = launched(what);
     if (st != AWE_OK) return st;
   }
   return AWE_OK;
 }
 
+template <class E>
+awe_status launch_type(const CacheLaunch& g, bool load, hipStream_t stream) {
+  const int patches = g.c.block / 4 * (g.c.head_dim / 8), threads = std::min(256, (patches + 63) / 64 * 64);
+  const char* what = load ? "cache load launch" : "cache store launch";
+  auto launch = [&](auto n) {
+    constexpr int k = decltype(n)::value;
+    return load ? launch_blocks(load_kernel<E, k>, g, threads, what, stream) : launch_blocks(store_kernel<E, k>, g, threads, what, stream);
+  };
+  return patches <= threads       ? launch(std::integral_constant<int, 1>{})
+         : patches <= 2 * threads ? launch(std::integral_constant<int, 2>{})
+                                  : launch(std::integral_constant<int, 4>{});  // 128 x 256 at most
+}
+awe_status launch_cache(const CacheLaunch& g, bool load, hipStream_t stream) {
+  return g.type == AWE_F32    ? launch_type<float>(g, load, stream)
+         : g.type == AWE_BF16 ? launch_type<bf16>(g, load, stream)
+                              : launch_type<f16>(g, load, stream);
+}
+
 }  // namespace
 
-awe_status launch_cache_store(const CacheLaunch& g, hipStream_t stream) {
-  const char* what = "cache store launch";
-  return g.type == AWE_F32    ? launch_tiles(store_kernel<float>, g, what, stream)
-         : g.type == AWE_BF16 ? launch_tiles(store_kernel<bf16>, g, what, stream)
-                              : launch_tiles(store_kernel<f16>, g, what, stream);
-}
-
-awe_status launch_cache_load(const CacheLaunch& g, hipStream_t stream) {
-  const char* what = "cache load launch";
-  return g.type == AWE_F32    ? launch_tiles(load_kernel<float>, g, what, stream)
-         : g.type == AWE_BF16 ? launch_tiles(load_kernel<bf16>, g, what, stream)
-                              : launch_tiles(load_kernel<f16>, g, what, stream);
-}
+awe_status launch_cache_store(const CacheLaunch& g, hipStream_t stream) { return launch_cache(g, false, stream); }
+awe_status launch_cache_load(const CacheLaunch& g, hipStream_t stream) { return launch_cache(g, true, stream); }
 
 namespace {
 template <awe_dtype T, int D>

@@ -120,6 +120,29 @@ def test_store_zero_tiny_and_non_finite(t):
     assert int(f) != 0
 
 
+@pytest.mark.parametrize("power", [-140, -126, -40, 0, 120])
+def test_store_rounds_quotients_as_the_definition(power):
+    # elements at and beside half steps of their scale, from subnormal scales to ones near the largest
+    heads, dim, block = 40, 256, 128
+    held = ref.Held(2, heads, dim, block, seed=6)
+    cache, table = upload(held), np.array([[1, 0]], dtype=np.int32)
+    rng = np.random.default_rng(power + 200)
+    rows = []
+    for _ in "kv":
+        most = (rng.uniform(1, 2, (2, heads)) * 2.0 ** power * 127).astype(np.float32)
+        x = (rng.integers(-127, 127, (2, block, heads, dim)) + 0.5) * (most / np.float32(127)).astype(np.float64)[:, None, :, None]
+        x = x.astype(np.float32)
+        to = rng.choice(np.array([-np.inf, 0, np.inf], dtype=np.float32), x.shape)
+        x = np.where(to == 0, x, np.nextafter(x, to))
+        x = np.clip(x, -most[:, None, :, None], most[:, None, :, None])
+        x[:, 5, :, 7] = most  # what sets the scale
+        rows.append(x.reshape(2 * block, heads, dim))
+    k, v = (torch.from_numpy(x).cuda() for x in rows)
+    awe.store_tokens(cache, batch_of([2 * block], [2 * block], table), k, v)
+    held.store(table[0], 2 * block, *rows)
+    same_cache(cache, held)
+
+
 def test_store_strides_and_rows_of_no_sequence():
     heads, dim, block, counts, lengths = 3, 64, 16, [4, 9], [20, 9]
     held = ref.Held(6, heads, dim, block, seed=5)
