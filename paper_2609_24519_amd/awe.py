@@ -9,6 +9,7 @@ falls back to another implementation.
 import ctypes
 import os
 import re
+import struct
 
 import numpy as np
 
@@ -287,8 +288,10 @@ def gemm_crt(M, N, K, A, lda, B, ldb, bound_a, bound_b, moduli, c128, c64, ldc, 
 
 
 # ---- quantised inference (cache and batch: Cache and Batch below, or their structures) ----------
-def _struct(x):
-    return ctypes.addressof(x if isinstance(x, ctypes.Structure) else x.struct) if x is not None else None
+def _struct(x):  # (bytes are passed as the address of their contents)
+    if isinstance(x, ctypes.Structure):
+        return ctypes.addressof(x)
+    return x.packed if x is not None else None
 
 
 def gemm_w4(M, N, K, X, ldx, x_type, x_scales, W, ldw, w_scales, lds, s_type, zeros, ldz, group, Y, ldy, y_type,
@@ -371,13 +374,18 @@ _types = {}  # torch dtype -> awe_dtype
 _torch = None  # both set when torch is first needed
 
 
-def _dtype(t, allowed):
+def _load_torch():
     global _torch
     if _torch is None:
         import torch
         _types.update({torch.int8: I8, torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16,
                        torch.int32: I32})
         _torch = torch
+
+
+def _dtype(t, allowed):
+    if _torch is None:
+        _load_torch()
     code = _types.get(t)
     if code not in allowed:
         raise ValueError("element type %s is not supported here" % t)
@@ -441,7 +449,7 @@ def matmul_w4(x, w, scales, group, zeros=None, x_scales=None, out_dtype=None):
     return y
 
 
-_INT8, _INT32, _FLOAT32 = (I8,), (I32,), (F32,)
+_INT32 = (I32,)
 
 
 class Cache:
@@ -449,23 +457,27 @@ class Cache:
     heads x dim x block) int8, k_scales and v_scales (blocks x heads) float32, all contiguous.  Keeps
     the tensors alive; ``Cache.empty`` allocates them."""
 
+    _layout = struct.Struct("@PPPPqiii0q")  # awe_cache
+
     def __init__(self, k, v, k_scales, v_scales):
-        if k.dim() != 4 or v.dim() != 4:
-            raise ValueError("k and v have four dimensions")
-        blocks, heads, block, dim = k.shape
-        if v.shape != (blocks, heads, dim, block) or _dtype(k.dtype, _INT8) != _dtype(v.dtype, _INT8):
+        try:
+            blocks, heads, block, dim = k.shape
+        except ValueError:
+            raise ValueError("k must be int8 of blocks x heads x block x dim") from None
+        _load_torch()
+        if k.dtype is not _torch.int8 or v.dtype is not _torch.int8 or v.shape != (blocks, heads, dim, block):
             raise ValueError("k must be int8 of blocks x heads x block x dim, v of blocks x heads x dim x block")
+        at, per_head = k.device, (blocks, heads)
         for s in (k_scales, v_scales):
-            if s.shape != (blocks, heads) or _dtype(s.dtype, _FLOAT32) != F32:
+            if s.dtype is not _torch.float32 or s.shape != per_head:
                 raise ValueError("scales must be float32 of blocks x heads")
-        at = k.device
         for t in (k, v, k_scales, v_scales):
             if not t.is_contiguous() or t.device != at:
                 raise ValueError("the cache's tensors must be contiguous, and on one device")
         self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
         self.heads, self.head_dim, self.block = heads, dim, block
-        self.struct = CacheStruct(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), blocks,
-                                  heads, dim, block)
+        self.packed = self._layout.pack(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(),
+                                        blocks, heads, dim, block)
 
     @classmethod
     def empty(cls, num_blocks, heads, head_dim, block, device="cuda"):
@@ -481,23 +493,32 @@ class Batch:
     (sequences x entries, rows with adjacent entries); rows, max_rows and max_length are plain numbers
     (the rows of the row tensors, and bounds).  Keeps the tensors alive."""
 
+    _layout = struct.Struct("@iPPPqqqq")  # awe_batch
+
     def __init__(self, starts, lengths, blocks, rows, max_rows, max_length):
-        n = lengths.shape[0]
-        for t in (starts, lengths, blocks):
-            _dtype(t.dtype, _INT32)
-        if starts.shape != (n + 1,) or lengths.dim() != 1 or blocks.dim() != 2 or blocks.shape[0] != n:
+        try:
+            (offsets,), (n,), (rows_of, entries), (ld, one) = starts.shape, lengths.shape, blocks.shape, blocks.stride()
+        except ValueError:
+            raise ValueError("starts and lengths must be vectors, blocks a matrix") from None
+        if offsets != n + 1 or rows_of != n:
             raise ValueError("starts, lengths and blocks must have sequences + 1, sequences and sequences rows")
+        _load_torch()
+        at, i32 = starts.device, _torch.int32
+        for t in (starts, lengths, blocks):
+            if t.dtype is not i32 or t.device != at:
+                raise ValueError("starts, lengths and blocks must be int32, and on one device")
         if not starts.is_contiguous() or not lengths.is_contiguous():
             raise ValueError("starts and lengths must be contiguous")
-        if lengths.device != starts.device or blocks.device != starts.device:
-            raise ValueError("starts, lengths and blocks must be on one device")
-        ld = _rows_2d(blocks, "blocks")
+        if (one != 1 and entries > 1) or (ld < entries and n > 1):
+            ld = _rows_2d(blocks, "blocks")  # (refuses it)
         self.starts, self.lengths, self.blocks, self.rows = starts, lengths, blocks, rows
-        # the last row holds blocks.shape[1] entries, so no position may lie past them
-        self.entries = blocks.shape[1]
-        self.max_length = max_length
-        self.struct = BatchStruct(n, starts.data_ptr(), lengths.data_ptr(), blocks.data_ptr(), ld, rows, max_rows,
-                                  max_length)
+        # the last row holds `entries` entries, so no position may lie past them
+        self.entries, self.max_length = entries, max_length
+        try:
+            self.packed = self._layout.pack(n, starts.data_ptr(), lengths.data_ptr(), blocks.data_ptr(),
+                                            ld if n > 1 else entries, rows, max_rows, max_length)
+        except struct.error:
+            raise ValueError("rows, max_rows and max_length must be whole numbers of 64 bits") from None
 
 
 def _row_tensor(t, cache, batch, heads, what):
