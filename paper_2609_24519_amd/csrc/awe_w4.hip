@@ -227,7 +227,7 @@ __device__ __forceinline__ float scale_value(uint32_t raw) {
   return (float)__builtin_bit_cast(_Float16, (uint16_t)raw);
 }
 
-// Few rows: 16 kN outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
+// Few rows, or few outputs: 16 kN outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
 // with up to kM x 16 rows of X.  Operands go straight from memory to the matrix unit, and a wave's loop is one
 // copy of the code for kD chunks, whose loads the compiler spreads over the products: unrolled
 // further to fetch ahead, it spent more time on fetching instructions than it saved (13.2 us instead of
@@ -685,7 +685,8 @@ awe_status launch_tile(const W4Args& a, int64_t tiles, hipStream_t stream) {
 template <awe_dtype T, int kFold>
 awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
   auto tiles = [&](int cols) { return ((a.g.M + 63) / 64) * ((a.g.N + cols - 1) / cols); };
-  // the widest tile that still gives each of the 256 CUs one; two workgroups per CU where there are enough
+  // the widest tile that still gives each of the 256 CUs one; two workgroups per CU where there are enough (four
+  // groups of waves on the narrowest tile: 47 us instead of 53 at 1024 x 1024 x 8192, but 90 instead of 77 at 1536 rows)
   if constexpr (kFold > 1) {  // (a fold at every step needs more registers than such a tile leaves)
     if (tiles(256) >= 512) return launch_tile<T, 4, 4, 1, kFold>(a, tiles(256), stream);
     if (tiles(256) >= 256) return launch_tile<T, 4, 4, 2, kFold>(a, tiles(256), stream);
@@ -696,7 +697,10 @@ awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
 
 template <awe_dtype T, int kFold>
 awe_status launch_kind(const W4Args& a, hipStream_t stream) {
-  if (a.g.M > 64) return launch_tiles<T, kFold>(a, stream);
+  // Up to 64 rows, and more while workgroups of 32 x 32 are at most two for each of the 256 CUs: these split the
+  // reduction over eight waves, a tile over two groups (BF16, K = 8192: 128 x 128 19 us instead of 43, 512 x 1024
+  // 43 instead of 52, but 1024 x 1024 80 instead of 53; K = 512: 4.5 / 8.8, 7.8 / 9.0, 13.4 / 9.3).
+  if (a.g.M > 64 && ((a.g.N + 31) / 32) * ((a.g.M + 31) / 32) > 512) return launch_tiles<T, kFold>(a, stream);
   // 16 outputs a workgroup while that is at most one per CU (M = 1: 8.4 us instead of 10.4 at 4096 x 8192,
   // but 12.3 instead of 10.9 at 8192 x 8192); beyond, 32 halve what is read of X
   const int rows = a.g.M <= 16 ? 16 : 32;

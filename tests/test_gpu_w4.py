@@ -51,7 +51,9 @@ def test_types_and_sizes(M, N, K, group, x, s, y, zeros):
 
 @pytest.mark.parametrize("x", ["bf16", "f16", "i8"])
 @pytest.mark.parametrize("M,N,K,group", [(1, 100, 1000, 32), (5, 64, 2048, 128), (33, 100, 777, 160), (64, 96, 512, 64),
-                                         (150, 140, 1111, 128), (256, 256, 1024, 32), (512, 384, 640, 640)])
+                                         (150, 140, 1111, 128), (256, 256, 1024, 32), (512, 384, 640, 640),
+                                         (150, 5000, 1111, 128), (256, 2200, 1024, 32), (100, 5300, 320, 64),
+                                         (800, 900, 384, 64), (1000, 650, 300, 512), (700, 790, 1024, 32)])
 @pytest.mark.parametrize("zeros", [False, True])
 def test_exact_sums(M, N, K, group, x, zeros):
     # small whole numbers and scales that are powers of two: every sum is exact in FP32, in any order
@@ -74,11 +76,11 @@ def test_many_outputs(M, N, K, group, x, zeros):
     check(d, group, "f32")
 
 
-@pytest.mark.parametrize("M", [1, 2, 16, 20, 50, 100, 300])
+@pytest.mark.parametrize("M,N", [(1, 75), (2, 75), (16, 75), (20, 75), (50, 75), (100, 75), (300, 75), (70, 6001), (300, 2005)])
 @pytest.mark.parametrize("x", ["bf16", "i8"])
-def test_strides_and_alignment(M, x):
+def test_strides_and_alignment(M, N, x):
     # every operand inside a larger buffer at odd offsets, with guards that must stay
-    N, K, group = 75, 333, 64
+    K, group = 333, 64
     G = -(-K // group)
     d = inputs(M, N, K, group, x, "f16", True, seed=M)
     want, bound = ref.w4(d["x"], d["w"], d["scales"], group, d["zeros"], d["x_scales"])
@@ -110,9 +112,9 @@ def test_empty_reduction_writes_zeros():
     assert awe.matmul_w4(x[:0], w, torch.zeros(9, 0, device="cuda"), 32).shape == (0, 9)
 
 
-@pytest.mark.parametrize("M", [4, 30, 100, 260])
-def test_nan_and_infinity_stay_in_their_row(M):
-    N, K, group = 140, 512, 128
+@pytest.mark.parametrize("M,N", [(4, 140), (30, 140), (100, 140), (260, 140), (100, 5200), (260, 2200)])
+def test_nan_and_infinity_stay_in_their_row(M, N):
+    K, group = 512, 128
     d = inputs(M, N, K, group, "bf16", "f32", False, seed=3)
     clean = check(d, group, "bf16")
     d["x"][1, 7] = float("nan")
@@ -124,10 +126,10 @@ def test_nan_and_infinity_stay_in_their_row(M):
 
 
 @pytest.mark.parametrize("x,power", [("bf16", -130), ("f16", -20)])
-@pytest.mark.parametrize("M", [3, 40, 100])
-def test_subnormal_rows(M, x, power):
+@pytest.mark.parametrize("M,N", [(3, 80), (40, 80), (100, 80), (100, 5200)])
+def test_subnormal_rows(M, N, x, power):
     # elements below the type's smallest normal number count in full
-    N, K, group = 80, 512, 128
+    K, group = 512, 128
     d = inputs(M, N, K, group, x, "f32", True, seed=4)
     d["x"][:] = (d["x"].float() * 2.0 ** power).to(T[x])
     d["scales"] *= 2.0 ** 60
@@ -136,8 +138,8 @@ def test_subnormal_rows(M, x, power):
 
 def test_scales_of_zero_and_far_apart():
     # a group whose scale is 0 adds nothing, whatever its neighbours' scales are
-    M, N, K, group = 80, 70, 512, 128
-    for m in (1, M):
+    K, group = 512, 128
+    for m, N in ((1, 70), (80, 70), (80, 5600)):
         d = inputs(m, N, K, group, "bf16", "f32", True, seed=5)
         d["scales"][:, 1] = 0
         d["scales"][::2, 2] = 2.0 ** 60
@@ -145,9 +147,9 @@ def test_scales_of_zero_and_far_apart():
         check(d, group, "f32")
 
 
-@pytest.mark.parametrize("M", [1, 48, 200])
-def test_rows_do_not_depend_on_the_others(M):
-    d = inputs(M, 130, 700, 64, "f16", "f32", True, seed=9)
+@pytest.mark.parametrize("M,N", [(1, 130), (48, 130), (200, 130), (200, 2500)])
+def test_rows_do_not_depend_on_the_others(M, N):
+    d = inputs(M, N, 700, 64, "f16", "f32", True, seed=9)
     a = check(d, 64, "f32")
     b = check(d, 64, "f32")
     assert torch.equal(a, b)
@@ -156,7 +158,8 @@ def test_rows_do_not_depend_on_the_others(M):
 
 
 def test_graph_replays_and_streams():
-    cases = [(1, 256, 512, 32, "bf16"), (20, 300, 512, 128, "i8"), (200, 300, 512, 128, "bf16")]
+    cases = [(1, 256, 512, 32, "bf16"), (20, 300, 512, 128, "i8"), (200, 300, 512, 128, "bf16"),
+             (200, 2500, 512, 128, "bf16")]
     sets = [(inputs(M, N, K, g, x, seed=i), g) for i, (M, N, K, g, x) in enumerate(cases)]
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
