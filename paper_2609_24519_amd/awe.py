@@ -371,6 +371,7 @@ def matmul_crt(A, B, moduli, bound_a, bound_b, d_range_flag=None):
 
 # ---- quantised inference on torch tensors ------------------------------------------------------
 _types = {}  # torch dtype -> awe_dtype
+_REAL, _REAL16, _REAL16_OR_INT8, _INT32 = (F32, BF16, F16), (BF16, F16), (BF16, F16, I8), (I32,)
 _torch = None  # both set when torch is first needed
 
 
@@ -392,18 +393,17 @@ def _dtype(t, allowed):
     return code
 
 
-def _on_current_device(*tensors):
-    """The library launches on the current device: its tensors must be there."""
-    here = -1
-    for t in tensors:
-        if t is None:
-            continue
-        at = t.get_device()
-        if at >= 0 and here < 0:
-            _current_stream()  # initialises CUDA the first time
-            here = _torch_c._cuda_getDevice() if _torch_c is not None else at
-        if at != here or at < 0:
+def _launch_stream(*tensors):
+    """Handle of the current stream; the library launches on the current device, so the tensors must be there."""
+    if _torch_c is None:
+        if any(t is not None and t.get_device() < 0 for t in tensors):
             raise ValueError("a tensor is not on the current device")
+        _current_stream()  # initialises CUDA the first time
+    here = _torch.cuda.current_device() if _torch_c is None else _torch_c._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("a tensor is not on the current device")
+    return _current_stream()
 
 
 def _rows_2d(t, what):
@@ -420,36 +420,43 @@ def matmul_w4(x, w, scales, group, zeros=None, x_scales=None, out_dtype=None):
     """Y = X W^T for CUDA tensors: x (M x K, bfloat16, float16 or int8), w (N x ceil(K / 2), uint8, two
     codes per byte, the low nibble first), scales and zeros (N x ceil(K / group); zeros uint8 or None
     for 8), x_scales (M float32, int8 x only).  out_dtype: x's type, bfloat16 for int8, if not given."""
-    ldx, ldw, lds = _rows_2d(x, "x"), _rows_2d(w, "w"), _rows_2d(scales, "scales")
-    M, K = x.shape
-    N, packed = w.shape
+    try:
+        ((M, K), (ldx, one)), ((N, packed), (ldw, w_one)), (lds, s_one) = \
+            (x.shape, x.stride()), (w.shape, w.stride()), scales.stride()
+    except ValueError:
+        raise ValueError("x, w and scales must be matrices") from None
     if group <= 0:
         raise ValueError("group must be positive")
     groups = -(-K // group)
-    x_type = _dtype(x.dtype, (BF16, F16, I8))
-    s_type = _dtype(scales.dtype, (F32, BF16, F16))
+    x_type = _dtype(x.dtype, _REAL16_OR_INT8)
+    s_type = _dtype(scales.dtype, _REAL)
     if out_dtype is None:
         out_dtype = _torch.bfloat16 if x_type == I8 else x.dtype
-    y_type = _dtype(out_dtype, (F32, BF16, F16))
-    if w.dtype != _torch.uint8 or packed != (K + 1) // 2:
+    y_type = _dtype(out_dtype, _REAL)
+    if w.dtype is not _torch.uint8 or packed != (K + 1) // 2:
         raise ValueError("w must be uint8 of N x ceil(K / 2)")
     if scales.shape != (N, groups):
         raise ValueError("scales must be N x ceil(K / group)")
+    # (anything but adjacent rows takes a closer look)
+    if one != 1 or ldx != K:
+        ldx = _rows_2d(x, "x")
+    if w_one != 1 or ldw != packed:
+        ldw = _rows_2d(w, "w")
+    if s_one != 1 or lds != groups:
+        lds = _rows_2d(scales, "scales")
     ldz = 0
     if zeros is not None:
         ldz = _rows_2d(zeros, "zeros")
-        if zeros.dtype != _torch.uint8 or zeros.shape != (N, groups):
+        if zeros.dtype is not _torch.uint8 or zeros.shape != (N, groups):
             raise ValueError("zeros must be uint8 of N x ceil(K / group)")
     if x_scales is not None and (x_scales.dtype != _torch.float32 or x_scales.shape != (M,)
                                  or not x_scales.is_contiguous()):
         raise ValueError("x_scales must be M float32 values")
-    _on_current_device(x, w, scales, zeros, x_scales)
+    stream = _launch_stream(x, w, scales, zeros, x_scales)
     y = x.new_empty((M, N), dtype=out_dtype)
-    gemm_w4(M, N, K, x, ldx, x_type, x_scales, w, ldw, scales, lds, s_type, zeros, ldz, group, y, N, y_type)
+    _check(lib().awe_gemm_w4(M, N, K, x.data_ptr(), ldx, x_type, _ptr(x_scales), w.data_ptr(), ldw, scales.data_ptr(),
+                             lds, s_type, _ptr(zeros), ldz, group, y.data_ptr(), N, y_type, stream), "awe_gemm_w4")
     return y
-
-
-_INT32 = (I32,)
 
 
 class Cache:
@@ -504,9 +511,9 @@ class Batch:
             raise ValueError("starts, lengths and blocks must have sequences + 1, sequences and sequences rows")
         _load_torch()
         at, i32 = starts.device, _torch.int32
-        for t in (starts, lengths, blocks):
-            if t.dtype is not i32 or t.device != at:
-                raise ValueError("starts, lengths and blocks must be int32, and on one device")
+        if (starts.dtype is not i32 or lengths.dtype is not i32 or blocks.dtype is not i32 or lengths.device != at
+                or blocks.device != at):
+            raise ValueError("starts, lengths and blocks must be int32, and on one device")
         if not starts.is_contiguous() or not lengths.is_contiguous():
             raise ValueError("starts and lengths must be contiguous")
         if (one != 1 and entries > 1) or (ld < entries and n > 1):
@@ -535,9 +542,10 @@ def _fits(cache, batch):
 
 
 def _flag(t):
-    if t is not None:
-        _dtype(t.dtype, _INT32)
-    return t
+    if t is None:
+        return None
+    _dtype(t.dtype, _INT32)
+    return t.data_ptr()
 
 
 def store_tokens(cache, batch, k, v, d_range_flag=None):
@@ -545,22 +553,24 @@ def store_tokens(cache, batch, k, v, d_range_flag=None):
     _fits(cache, batch)
     k_row, k_head = _row_tensor(k, cache, batch, cache.heads, "k")
     v_row, v_head = _row_tensor(v, cache, batch, cache.heads, "v")
-    if k.dtype != v.dtype:
+    if k.dtype is not v.dtype:
         raise ValueError("k and v have different types")
-    _on_current_device(cache.k, batch.starts, k, v, _flag(d_range_flag))
-    cache_store(cache, batch, k, k_row, k_head, v, v_row, v_head, _dtype(k.dtype, (F32, BF16, F16)), d_range_flag)
+    flag, stream = _flag(d_range_flag), _launch_stream(cache.k, batch.starts, k, v, d_range_flag)
+    _check(lib().awe_cache_store(cache.packed, batch.packed, k.data_ptr(), k_row, k_head, v.data_ptr(), v_row, v_head,
+                                 _dtype(k.dtype, _REAL), flag, stream), "awe_cache_store")
 
 
 def load_tokens(cache, batch, dtype, d_range_flag=None):
     """(k, v), rows x heads x dim of dtype: what the newest tokens of the batch's sequences stand for.
     Rows that belong to no sequence are not written."""
-    import torch
     _fits(cache, batch)
-    _on_current_device(cache.k, batch.starts, _flag(d_range_flag))
-    shape = (batch.rows, cache.heads, cache.head_dim)
-    k, v = (torch.empty(shape, dtype=dtype, device=cache.k.device) for _ in range(2))
-    row, head = shape[1] * shape[2], shape[2]
-    cache_load(cache, batch, k, row, head, v, row, head, _dtype(dtype, (F32, BF16, F16)), d_range_flag)
+    code = _dtype(dtype, _REAL)
+    flag, stream = _flag(d_range_flag), _launch_stream(cache.k, batch.starts, d_range_flag)
+    heads, dim = cache.heads, cache.head_dim
+    k = cache.k.new_empty((batch.rows, heads, dim), dtype=dtype)
+    v = _torch.empty_like(k)
+    _check(lib().awe_cache_load(cache.packed, batch.packed, k.data_ptr(), heads * dim, dim, v.data_ptr(), heads * dim,
+                                dim, code, flag, stream), "awe_cache_load")
     return k, v
 
 
@@ -570,15 +580,24 @@ def attend(cache, batch, q, scale, causal=True, out=None, d_range_flag=None):
     _fits(cache, batch)
     heads = q.shape[1] if q.dim() == 3 else 0
     q_row, q_head = _row_tensor(q, cache, batch, heads, "q")
-    dtype = _dtype(q.dtype, (BF16, F16))
+    dtype = _dtype(q.dtype, _REAL16)
+    if out is not None:
+        if out.dtype is not q.dtype:
+            raise ValueError("out and q have different types")
+        out_row, out_head = _row_tensor(out, cache, batch, heads, "out")
+    flag, stream = _flag(d_range_flag), _launch_stream(cache.k, batch.starts, q, out, d_range_flag)
     if out is None:
-        out = q.new_empty(q.shape)
-    elif out.dtype != q.dtype:
-        raise ValueError("out and q have different types")
-    out_row, out_head = _row_tensor(out, cache, batch, heads, "out")
-    _on_current_device(cache.k, batch.starts, q, out, _flag(d_range_flag))
-    n = cache_attend_workspace_bytes(cache, batch, heads)
-    ws = q.new_empty(n, dtype=_torch.uint8) if n else None
-    cache_attend(cache, batch, q, q_row, q_head, heads, dtype, scale, 1 if causal else 0, out, out_row, out_head, ws,
-                 n, d_range_flag)
+        out = _torch.empty_like(q) if q.is_contiguous() else q.new_empty(q.shape)
+        out_row, out_head = heads * cache.head_dim, cache.head_dim
+
+    def call(ws, n):
+        return lib().awe_cache_attend(cache.packed, batch.packed, q.data_ptr(), q_row, q_head, heads, dtype, scale,
+                                      1 if causal else 0, out.data_ptr(), out_row, out_head, ws, n, flag, stream)
+    # most calls need no workspace; those that do are refused, before anything is enqueued
+    st = call(None, 0)
+    if st == ERR_WORKSPACE:
+        n = cache_attend_workspace_bytes(cache, batch, heads)
+        ws = q.new_empty(n, dtype=_torch.uint8)
+        st = call(ws.data_ptr(), n)
+    _check(st, "awe_cache_attend")
     return out
