@@ -229,9 +229,10 @@ __device__ __forceinline__ float scale_value(uint32_t raw) {
 
 // Few rows, or few outputs: 16 kN outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
 // with up to kM x 16 rows of X.  Operands go straight from memory to the matrix unit, and a wave's loop is one
-// copy of the code for kD chunks, whose loads the compiler spreads over the products: unrolled
-// further to fetch ahead, it spent more time on fetching instructions than it saved (13.2 us instead of
-// 10.6 for one row at 8192 x 8192; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
+// copy of the code for kD chunks, whose loads the compiler spreads over the products.  Bound by the weights' bytes
+// and the loads' latency: one row at 8192 x 8192 takes 11.2 us (35 MB, 3.1 TB/s), 16 int8 rows 12.6.  Unrolled
+// further to fetch ahead, it spends more time on fetching instructions than it saves (13.2 us for one
+// row; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
 constexpr int kW = 8;
 
 template <awe_dtype T, int kM, int kN, int kD, int kFold, awe_dtype S>
@@ -405,7 +406,9 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 // row, -(bias + 8) sum x over a group, which is where a group's sum starts; scales and zero points lie there
 // too, as floats.  A wave's weights go from memory to its registers, and no other wave unpacks them.
 // kG groups of four waves take the chunks in turn, each with X of its own in LDS, and add up at the end, so that
-// a CU with one workgroup has two waves per SIMD, too.
+// a CU with one workgroup has two waves per SIMD, too.  Bound by vector instructions (half the cycles, for
+// the codes and the folding; MFMAs take a third), at the two waves per SIMD that the registers allow: BF16 rows
+// against 8192 x 8192 take 93 us for 512 (740 TFLOP/s) and 715-760 for 4096 (720-770; a plain product of BF16 numbers reaches 1250).
 template <awe_dtype T, int kM, int kN, int kFold>
 struct TileLds {  // of a group of waves
   using X = Kind<T>;
