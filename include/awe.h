@@ -300,7 +300,7 @@ awe_status awe_gemm_crt(int64_t M, int64_t N, int64_t K, const int64_t* A, int64
      Y[i,j] = x_scales[i] * sum_g w_scales[j,g] * sum_{k in group g} X[i,k] * (u[j,k] - z[j,g]).
    X is M x K (x_type AWE_BF16, AWE_F16 or AWE_I8, leading dimension ldx).  Row j of W holds the
    codes u[j,k] in 0..15 of output j: byte W[j*ldw + k/2], the low nibble for even k, ldw >=
-   ceil(K/2) bytes (at an odd K the last high nibble is ignored; rows at odd addresses take longer).  Group g covers indices
+   ceil(K/2) bytes (at an odd K the last high nibble is ignored; rows off 4-byte addresses take longer).  Group g covers indices
    g*group .. g*group + group - 1; group is a multiple of 32, or at least K (one group); the last
    group may be short.  w_scales[j*lds + g] has s_type (AWE_F32, AWE_BF16, AWE_F16), zero points
    zeros[j*ldz + g] are bytes, and NULL stands for 8 everywhere (codes of -8..7).  x_scales: FP32, for

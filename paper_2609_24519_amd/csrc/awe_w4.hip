@@ -227,6 +227,31 @@ __device__ __forceinline__ float scale_value(uint32_t raw) {
   return (float)__builtin_bit_cast(_Float16, (uint16_t)raw);
 }
 
+// Bytes of a row as they are loaded.  kOdd: at any address, as the words that hold them (the last one may be one
+// more), put together when they are used; the memory system takes about twice as long for wide loads at addresses
+// that are not multiples of 4.
+template <int kBytes, bool kOdd>
+struct Piece {
+  static constexpr int kN = kBytes / 4;
+  struct Aligned {
+    uint32_t w[kN];
+  };
+  uint32_t w[kN + (kOdd ? 1 : 0)];
+
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    const Aligned a = *reinterpret_cast<const Aligned*>(kOdd ? at & ~uintptr_t(3) : at);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) w[i] = a.w[i];
+    if constexpr (kOdd) w[kN] = *reinterpret_cast<const uint32_t*>((at + kBytes - 1) & ~uintptr_t(3));
+  }
+  __device__ __forceinline__ uint32_t word(int i, uint32_t shift) const {  // shift: the address modulo 4
+    if constexpr (kOdd) return __builtin_amdgcn_alignbyte(w[i + 1], w[i], shift);
+    return w[i];
+  }
+};
+__device__ __forceinline__ uint32_t in_word(const uint8_t* p) { return (uint32_t)reinterpret_cast<uintptr_t>(p) & 3; }
+
 // Few rows, or few outputs: 16 kN outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
 // with up to kM x 16 rows of X.  Operands go straight from memory to the matrix unit, and a wave's loop is one
 // copy of the code for kD chunks, whose loads the compiler spreads over the products.  Bound by the weights' bytes
@@ -235,15 +260,21 @@ __device__ __forceinline__ float scale_value(uint32_t raw) {
 // row; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
 constexpr int kW = 8;
 
-template <awe_dtype T, int kM, int kN, int kD, int kFold, awe_dtype S>
+// S: the scales' type, or kAnyScale for the one that the call says (one row at 8192 x 8192: 14.1 us instead of 11.2).
+// kOddX, kOddW: rows of X or W that begin off 4-byte addresses.
+constexpr awe_dtype kAnyScale = AWE_I32;
+
+template <awe_dtype T, int kM, int kN, int kD, int kFold, awe_dtype S, bool kOddX, bool kOddW>
 __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   using X = Kind<T>;
   using Elem = typename X::Elem;
   constexpr int kUnits = 4 / kFold;  // of a chunk
   constexpr bool kPairs = T == AWE_I8 && kFold > 1;
   constexpr int kS = kFold < 4 ? kD : 1;
-  constexpr int kE = sizeof(Elem), kSE = S == AWE_F32 ? 4 : 2;
+  constexpr int kE = sizeof(Elem), kLoads = kPairs ? 2 : 4, kLoad = 128 * kE / 4 / kLoads;  // of X, in a chunk: bytes each
   const W4Launch& g = a.g;
+  const awe_dtype s_type = S == kAnyScale ? g.s_type : S;
+  const int s_bytes = s_type == AWE_F32 ? 4 : 2;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane >> 4, i = lane & 15;
   const int64_t n0 = (int64_t)blockIdx.x * 16 * kN, m0 = (int64_t)blockIdx.y * 16 * kM;
 
@@ -251,7 +282,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   // the last row or output, that one again: its result is not stored.
   const bool has_z = g.zeros != nullptr;
   const uint8_t* wb = g.w + n0 * g.ldw;
-  const uint8_t* sb = reinterpret_cast<const uint8_t*>(g.scales) + n0 * g.lds * kSE;
+  const uint8_t* sb = reinterpret_cast<const uint8_t*>(g.scales) + n0 * g.lds * s_bytes;
   const uint8_t* zb = has_z ? g.zeros + n0 * g.ldz : g.w;  // (any byte, where there are none)
   const uint8_t* xb = reinterpret_cast<const uint8_t*>(g.x) + m0 * g.ldx * kE;
   uint32_t wo[kN], so[kN], zo[kN], xo[kM];
@@ -259,7 +290,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
   for (int t = 0; t < kN; ++t) {
     const uint32_t n = (uint32_t)std::min<int64_t>(16 * t + i, g.N - 1 - n0);
     wo[t] = n * (uint32_t)g.ldw + 16 * q;
-    so[t] = n * (uint32_t)g.lds * kSE;
+    so[t] = n * (uint32_t)g.lds * s_bytes;
     zo[t] = has_z ? n * (uint32_t)g.ldz : 0;
   }
 #pragma unroll
@@ -299,7 +330,9 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
       for (int t = 0; t < kN; ++t) {
         const int from = 16 * (kFold < 4 ? j : of) + i;
-        const float sc = scale_value<S>(__shfl(s[t], from)), b = X::kBias + (has_z ? (float)__shfl(z[t], from) : 8.f);
+        const uint32_t raw = __shfl(s[t], from);
+        const float sc = s_type == AWE_F32 ? scale_value<AWE_F32>(raw) : s_type == AWE_BF16 ? scale_value<AWE_BF16>(raw) : scale_value<AWE_F16>(raw);
+        const float b = X::kBias + (has_z ? (float)__shfl(z[t], from) : 8.f);
 #pragma unroll
         for (int u = 0; u < kM; ++u)
 #pragma unroll
@@ -313,24 +346,22 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
     const int32_t grp = std::min((int32_t)(unit / (uint32_t)a.units), last);
 #pragma unroll
     for (int t = 0; t < kN; ++t) {
-      s[t] = raw_scale<S>(sb + (so[t] + (uint32_t)grp * kSE));
+      const uint8_t* p = sb + (so[t] + (uint32_t)grp * s_bytes);
+      s[t] = s_type == AWE_F32 ? raw_scale<AWE_F32>(p) : raw_scale<AWE_F16>(p);
       z[t] = zb[zo[t] + (has_z ? (uint32_t)grp : 0)];
     }
   };
 
 #pragma unroll 1
   for (int32_t c0 = wave; c0 < full; c0 += kW * kD) {  // chunks c0 + u kW
-    u4 cw[kD][kN];
-    typename X::Raw xr[kD][kM][4];
+    Piece<16, kOddW> cw[kD][kN];
+    Piece<kLoad, kOddX> xr[kD][kM][kLoads];
     uint32_t s[kS][kN], z[kS][kN];
 #pragma unroll
     for (int u = 0; u < kD; ++u) {
       const int64_t c = std::min(c0 + u * kW, full - 1);  // (past the end: the last one again, unused)
 #pragma unroll
-      for (int t = 0; t < kN; ++t) {
-        const Any16 v = *reinterpret_cast<const Any16*>(wb + c * (kChunk / 2) + wo[t]);
-        cw[u][t] = u4{v.w[0], v.w[1], v.w[2], v.w[3]};
-      }
+      for (int t = 0; t < kN; ++t) cw[u][t].load(wb + c * (kChunk / 2) + wo[t]);
     }
     // quarter q fetches the scales of the q-th chunk (of step q of each, where it has several)
 #pragma unroll
@@ -341,21 +372,35 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
       for (int t = 0; t < kM; ++t)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint8_t* p = xb + (c * kChunk + step_offset<kPairs>(0, j)) * kE + xo[t];
-          if constexpr (!kPairs) {
-            xr[u][t][j] = load8<T>(reinterpret_cast<const Elem*>(p));
-          } else if (j % 2 == 0) {
-            const Any16 v = *reinterpret_cast<const Any16*>(p);
-            xr[u][t][j] = (uint64_t)v.w[0] | (uint64_t)v.w[1] << 32;
-            xr[u][t][j + 1] = (uint64_t)v.w[2] | (uint64_t)v.w[3] << 32;
-          }
-        }
+        for (int j = 0; j < kLoads; ++j) xr[u][t][j].load(xb + (c * kChunk + step_offset<kPairs>(0, j * (4 / kLoads))) * kE + xo[t]);
     }
 #pragma unroll
     for (int u = 0; u < kD; ++u) {
       if (c0 + u * kW >= full) break;
-      chunk(cw[u], xr[u], s[kFold < 4 ? u : 0], z[kFold < 4 ? u : 0], u);
+      u4 codes[kN];
+      typename X::Raw rows[kM][4];
+#pragma unroll
+      for (int t = 0; t < kN; ++t) {
+        const uint32_t shift = in_word(wb + wo[t]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) codes[t][i] = cw[u][t].word(i, shift);
+      }
+#pragma unroll
+      for (int t = 0; t < kM; ++t) {
+        const uint32_t shift = in_word(xb + xo[t]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (T == AWE_I8) {
+            const int first = kPairs ? 2 * (j & 1) : 0;
+            const Piece<kLoad, kOddX>& p = xr[u][t][kPairs ? j / 2 : j];
+            rows[t][j] = (uint64_t)p.word(first, shift) | (uint64_t)p.word(first + 1, shift) << 32;
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rows[t][j][i] = xr[u][t][j].word(i, shift);
+          }
+        }
+      }
+      chunk(codes, rows, s[kFold < 4 ? u : 0], z[kFold < 4 ? u : 0], u);
     }
   }
 
@@ -662,12 +707,21 @@ awe_status launch_rows(const W4Args& a, hipStream_t stream) {
   const dim3 block(64 * kW);
   if ((int64_t)grid.x * block.x >= int64_t(1) << 32) return too_many();
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, stream, a); };
-  if (a.g.s_type == AWE_F32)
-    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F32>);
+  // Rows off 4-byte addresses are loaded as words and put together (33 FP16 rows, 1537 outputs, K = 2049: 9 us
+  // instead of 17; one row against odd rows of W, 8192 x 8192: 15 instead of 21); X's alone are not told apart from both.
+  auto odd = [](const void* p, int64_t rows, int64_t stride) {
+    return reinterpret_cast<uintptr_t>(p) % 4 != 0 || (rows > 1 && stride % 4 != 0);
+  };
+  if (odd(a.g.x, a.g.M, a.g.ldx * (int64_t)sizeof(typename Kind<T>::Elem)))
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, kAnyScale, true, true>);
+  else if (odd(a.g.w, a.g.N, a.g.ldw))
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, kAnyScale, false, true>);
+  else if (a.g.s_type == AWE_F32)
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F32, false, false>);
   else if (a.g.s_type == AWE_BF16)
-    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_BF16>);
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_BF16, false, false>);
   else
-    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F16>);
+    launch(w4_rows_kernel<T, kM, kN, kD, kFold, AWE_F16, false, false>);
   return launched("w4 launch");
 }
 

@@ -101,6 +101,30 @@ def test_strides_and_alignment(M, N, x):
         assert bool((Y[:, N:] == 7).all()) and bool((guard[:lead] == 7).all()) and bool((guard[-8:] == 7).all())
 
 
+@pytest.mark.parametrize("x", ["bf16", "f16", "i8"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N", [(1, 40), (9, 5000), (33, 4200), (70, 200)])
+@pytest.mark.parametrize("lead_x,extra_x,lead_w,extra_w", [(0, 1, 0, 0), (1, 4, 0, 4), (0, 4, 0, 1), (4, 8, 1, 4), (3, 2, 2, 2)])
+def test_rows_off_words(M, N, group, x, lead_x, extra_x, lead_w, extra_w):
+    # every way in which rows of X and W lie off multiples of 4 bytes; all sums are exact
+    K = 1096
+    g = torch.Generator().manual_seed(M + group + lead_x)
+    d = inputs(M, N, K, group, "i8", "f32", True, x_scales=False, seed=M)
+    d["x"] = torch.randint(-4, 5, (M, K), generator=g).to(T[x]).cuda()
+    d["scales"] = torch.tensor([0.25, 0.5, 1.0, 2.0])[torch.randint(0, 4, d["scales"].shape, generator=g)].cuda()
+
+    def inside(t, lead, extra):
+        big = torch.zeros(lead + t.shape[0] * (t.shape[1] + extra), dtype=t.dtype, device="cuda")
+        v = big[lead:].view(t.shape[0], t.shape[1] + extra)[:, : t.shape[1]]
+        v.copy_(t)
+        return v
+
+    got = awe.matmul_w4(inside(d["x"], lead_x, extra_x), inside(d["w"], lead_w, extra_w), d["scales"], group, d["zeros"],
+                        None, torch.float32)
+    want, _ = ref.w4(d["x"], d["w"], d["scales"], group, d["zeros"])
+    assert np.abs(want).max() * 4 < 2 ** 22 and np.array_equal(ref.f64(got), want)
+
+
 def test_empty_reduction_writes_zeros():
     for M in (1, 70):
         x, w = torch.zeros(M, 0, dtype=torch.bfloat16, device="cuda"), torch.zeros(9, 0, dtype=torch.uint8, device="cuda")
