@@ -304,11 +304,10 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 
   // A chunk's products.  s, z: a lane's scale and zero point of output tile t, in the quarter that fetched
   // it: the step's, or `of` where a chunk lies in one group.
-  auto chunk = [&](const u4 (&cw)[kN], const typename X::Raw (&xr)[kM][4], const uint32_t (&s)[kN], const uint32_t (&z)[kN],
-                   int of) {
+  auto chunk = [&](auto codes, auto row, const uint32_t (&s)[kN], const uint32_t (&z)[kN], int of) {
     u4 c[kN];
 #pragma unroll
-    for (int t = 0; t < kN; ++t) c[t] = kPairs ? across_quarters_by_16(cw[t]) : across_quarters(cw[t]);
+    for (int t = 0; t < kN; ++t) c[t] = kPairs ? across_quarters_by_16(codes(t)) : across_quarters(codes(t));
     typename X::Acc part[kN][kM], sum[kM];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -316,7 +315,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
       typename X::Op e[kM];
 #pragma unroll
       for (int u = 0; u < kM; ++u) {
-        e[u] = X::elems(xr[u][j]);
+        e[u] = X::elems(row(u, j));
         sum[u] = X::mul(e[u], X::ones(), first ? X::zero() : sum[u]);
       }
 #pragma unroll
@@ -377,30 +376,22 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
     for (int u = 0; u < kD; ++u) {
       if (c0 + u * kW >= full) break;
-      u4 codes[kN];
-      typename X::Raw rows[kM][4];
-#pragma unroll
-      for (int t = 0; t < kN; ++t) {
+      auto codes = [&](int t) {
         const uint32_t shift = in_word(wb + wo[t]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) codes[t][i] = cw[u][t].word(i, shift);
-      }
-#pragma unroll
-      for (int t = 0; t < kM; ++t) {
+        const Piece<16, kOddW>& p = cw[u][t];
+        return u4{p.word(0, shift), p.word(1, shift), p.word(2, shift), p.word(3, shift)};
+      };
+      auto row = [&](int t, int j) {
         const uint32_t shift = in_word(xb + xo[t]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if constexpr (T == AWE_I8) {
-            const int first = kPairs ? 2 * (j & 1) : 0;
-            const Piece<kLoad, kOddX>& p = xr[u][t][kPairs ? j / 2 : j];
-            rows[t][j] = (uint64_t)p.word(first, shift) | (uint64_t)p.word(first + 1, shift) << 32;
-          } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rows[t][j][i] = xr[u][t][j].word(i, shift);
-          }
+        const Piece<kLoad, kOddX>& p = xr[u][t][kPairs ? j / 2 : j];
+        if constexpr (T == AWE_I8) {
+          const int first = kPairs ? 2 * (j & 1) : 0;
+          return (uint64_t)p.word(first, shift) | (uint64_t)p.word(first + 1, shift) << 32;
+        } else {
+          return u4{p.word(0, shift), p.word(1, shift), p.word(2, shift), p.word(3, shift)};
         }
-      }
-      chunk(codes, rows, s[kFold < 4 ? u : 0], z[kFold < 4 ? u : 0], u);
+      };
+      chunk(codes, row, s[kFold < 4 ? u : 0], z[kFold < 4 ? u : 0], u);
     }
   }
 
@@ -420,7 +411,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
         xr[t][j] = load8_end<T>(row, k0 + step_offset<kPairs>(q, j), g.K);
       }
     scales(kFold < 4 ? kUnits * full + q / kFold : full, s, z);
-    chunk(cw, xr, s, z, 0);
+    chunk([&](int t) { return cw[t]; }, [&](int t, int j) { return xr[t][j]; }, s, z, 0);
   }
 
   __shared__ struct {
