@@ -364,6 +364,34 @@ def test_attend_strides_and_rows_of_no_sequence():
     ref.close(o[5:45], w, e, torch.bfloat16)
 
 
+@pytest.mark.parametrize("counts,lengths,wide", [([1, 1], [300, 5], False), ([1], [5000], False), ([40, 260], [300, 260], True)])
+def test_offsets_past_32_bits(counts, lengths, wide):
+    # the same tokens in a small cache and in the last blocks of one of 5 GiB each for keys and values
+    heads, dim, block, share, far = 8, 256, 128, 2, 20480
+    per = [-(-n // block) for n in lengths]
+    table = np.zeros((len(lengths), max(per)), dtype=np.int32)
+    ids = iter(range(sum(per)))
+    for i, n in enumerate(per):
+        table[i, :n] = [next(ids) for _ in range(n)]
+    g = torch.Generator().manual_seed(8)
+    every, rows = sum(lengths), sum(counts)
+    k, v = (torch.randn(every, heads, dim, generator=g).bfloat16().cuda() for _ in "kv")
+    q = torch.randn(WIDE if wide else rows, heads * share, dim, generator=g).bfloat16().cuda()
+    bounds = dict(rows=WIDE, max_rows=WIDE) if wide else {}
+    results = []
+    for blocks, first in ((sum(per), 0), (far, far - sum(per))):
+        cache = awe.Cache.empty(blocks, heads, dim, block)
+        at = table + first
+        awe.store_tokens(cache, batch_of(lengths, lengths, at), k, v)
+        out = torch.zeros_like(q)
+        awe.attend(cache, batch_of(counts, lengths, at, **bounds), q, dim ** -0.5, out=out)
+        results.append((out, *awe.load_tokens(cache, batch_of(lengths, lengths, at), torch.bfloat16)))
+        del cache
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert bool(results[0][0][:rows].any())
+
+
 def test_attend_workspace_refused_when_small():
     lengths = [9000]
     held = ref.Held(150, 1, 64, 64, seed=18)

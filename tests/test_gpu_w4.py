@@ -125,6 +125,22 @@ def test_rows_off_words(M, N, group, x, lead_x, extra_x, lead_w, extra_w):
     assert np.abs(want).max() * 4 < 2 ** 22 and np.array_equal(ref.f64(got), want)
 
 
+@pytest.mark.parametrize("M,N", [(3, 40), (40, 700), (70, 7800)])
+def test_offsets_past_32_bits(M, N):
+    # rows of W and Y so far apart that the last ones lie past 4 GiB
+    K, group = 384, 128
+    d = inputs(M, N, K, group, "bf16", "f32", True, seed=N)
+    ldw = min((1 << 24) - 4, ((5 << 30) // N + 3) // 4 * 4)
+    big = torch.empty(N * ldw, dtype=torch.uint8, device="cuda")
+    w = big.view(N, ldw)[:, : K // 2]
+    w.copy_(d["w"])
+    ldy = (5 << 30) // 2 // M
+    y = torch.empty(M * ldy, dtype=torch.bfloat16, device="cuda").view(M, ldy)[:, :N]
+    awe.gemm_w4(M, N, K, d["x"], K, awe.BF16, None, w, ldw, d["scales"], 3, awe.F32, d["zeros"], 3, group, y, ldy, awe.BF16)
+    want, bound = ref.w4(d["x"], d["w"], d["scales"], group, d["zeros"])
+    ref.close(y, want, bound, torch.bfloat16)
+
+
 def test_empty_reduction_writes_zeros():
     for M in (1, 70):
         x, w = torch.zeros(M, 0, dtype=torch.bfloat16, device="cuda"), torch.zeros(9, 0, dtype=torch.uint8, device="cuda")
