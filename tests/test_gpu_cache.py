@@ -277,6 +277,23 @@ def test_attend_long_sequences_split(share, new):
                max_length=60000)
 
 
+@pytest.mark.parametrize("new,wide", [(1, False), (30, False), (30, True)])
+def test_attend_shared_and_repeated_blocks(new, wide):
+    # sequences with a common beginning, and one whose table names a block twice
+    lengths, block = [300, 290, 333, 5000 if not wide else 400], 32
+    held = ref.Held(160, 2, 128, block, seed=15)
+    table = np.random.default_rng(3).integers(0, 160, (4, 160)).astype(np.int32)
+    table[1, :8] = table[0, :8]
+    table[2, 5] = table[2, 2]
+    table[3, :10] = table[2, :10]
+    run_attend(held, table, [new] * 4, lengths, 4, "bf16", True, wide=wide)
+    # rows of one sequence as two sequences of the call: the same tokens, the same results
+    got, q, _ = run_attend(held, table[:1], [2], [200], 4, "f16", False, wide=wide)
+    twice, _, _ = run_attend(held, table[[0, 0]], [1, 1], [200, 200], 4, "f16", False, wide=wide)
+    if not wide:  # (a column's sums do not depend on its tile)
+        assert torch.equal(got, twice)
+
+
 @pytest.mark.parametrize("new,wide", [(1, False), (40, False), (40, True)])
 def test_attend_blocks_of_very_different_scales(new, wide):
     # one block of large values that gets no weight must not cost the others their digits
