@@ -288,25 +288,26 @@ awe_status awe_gemm_crt(int64_t M, int64_t N, int64_t K, const int64_t* A, int64
                         hipStream_t stream);
 
 /* ---- Quantised inference -----------------------------------------------------------------
-   Products with 4-bit weights that carry a scale per group, and attention over keys and values
-   held in 8 bits.  Integers are multiplied as integers or as floating-point numbers that hold them
-   exactly; sums, scales and softmax statistics are FP32, and each result is rounded once to its
-   type (nearest, ties to even).  Results are the same on every run and do not depend on a call's
-   other rows, except that the sizes select the kernel and with it the order of sums.  The calls
-   enqueue only kernels, allocate nothing and keep nothing: they can be captured into a graph at
-   any time, and overlap on any streams as long as no call writes what another uses.  Outputs share no memory with inputs or a workspace. */
+   Products with 4-bit weights that carry a scale per group, and attention over keys and values held in
+   8 bits.  Integers are multiplied as integers or as floating-point numbers that hold them exactly;
+   sums, scales and softmax statistics are FP32, and each result is rounded once to its type (nearest,
+   ties to even).  Results are the same on every run and do not depend on a call's other rows, except
+   that the sizes select the kernel and with it the order of sums.  The calls enqueue only kernels,
+   allocate nothing and keep nothing: they can be captured into a graph at any time, and overlap on any
+   streams as long as no call writes what another uses.  Outputs share no memory with inputs or a
+   workspace. */
 
 /* Y = X W^T with 4-bit weights: for i < M, j < N
      Y[i,j] = x_scales[i] * sum_g w_scales[j,g] * sum_{k in group g} X[i,k] * (u[j,k] - z[j,g]).
-   X is M x K (x_type AWE_BF16, AWE_F16 or AWE_I8, leading dimension ldx).  Row j of W holds the
-   codes u[j,k] in 0..15 of output j: byte W[j*ldw + k/2], the low nibble for even k, ldw >=
-   ceil(K/2) bytes (at an odd K the last high nibble is ignored; rows off 4-byte addresses take longer).  Group g covers indices
-   g*group .. g*group + group - 1; group is a multiple of 32, or at least K (one group); the last
-   group may be short.  w_scales[j*lds + g] has s_type (AWE_F32, AWE_BF16, AWE_F16), zero points
-   zeros[j*ldz + g] are bytes, and NULL stands for 8 everywhere (codes of -8..7).  x_scales: FP32, for
-   AWE_I8 only, NULL for 1.  Y is M x N of y_type (AWE_F32, AWE_BF16, AWE_F16).  Pointers are aligned to
-   their element; rows may begin anywhere, less than 16 MiB apart.  K = 0 writes zeros.  A NaN or infinity in a row of X
-   reaches that row of Y alone. */
+   X is M x K (x_type AWE_BF16, AWE_F16 or AWE_I8, leading dimension ldx).  Row j of W holds the codes
+   u[j,k] in 0..15 of output j: byte W[j*ldw + k/2], the low nibble for even k, ldw >= ceil(K/2) bytes
+   (at an odd K the last high nibble is ignored; rows off 4-byte addresses take longer).  Group g
+   covers indices g*group .. g*group + group - 1; group is a multiple of 32, or at least K (one group);
+   the last group may be short.  w_scales[j*lds + g] has s_type (AWE_F32, AWE_BF16, AWE_F16), zero
+   points zeros[j*ldz + g] are bytes, and NULL stands for 8 everywhere (codes of -8..7).  x_scales:
+   FP32, for AWE_I8 only, NULL for 1.  Y is M x N of y_type (AWE_F32, AWE_BF16, AWE_F16).  Pointers are
+   aligned to their element; rows may begin anywhere, less than 16 MiB apart.  K = 0 writes zeros.  A
+   NaN or infinity in a row of X reaches that row of Y alone. */
 awe_status awe_gemm_w4(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, awe_dtype x_type,
                        const float* x_scales, const uint8_t* W, int64_t ldw, const void* w_scales, int64_t lds,
                        awe_dtype s_type, const uint8_t* zeros, int64_t ldz, int64_t group, void* Y, int64_t ldy,
