@@ -287,6 +287,7 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;     // per workgroup
 constexpr int kTokens = 64;   // per step of a wave
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLargeScore = 1024.f;
 
 union Halves {
   h8 v;
@@ -307,6 +308,12 @@ __device__ __forceinline__ h8 widen(uint32_t a, uint32_t b) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) r.p[i] += less;
   return r.v;
+}
+
+// A product rounded by itself, never within a fused multiply-add.
+__device__ __forceinline__ float product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
 }
 
 // Largest over the four quarters of a column (NaN is passed over; it shows in the sum).
@@ -396,6 +403,9 @@ struct Columns {
   // weights.  They lie in one block, so the weights times its values' scale, w = vs 2^(15 - e) < 2^15, are exp2 of
   // one linear function of the scores, and the weights' sum is theirs over w.  FP16 keeps 11 bits of what is
   // at least 2^-29 of the largest scale so far, and to 2^-40 of it of the rest.
+  // The running maximum is a rounded product.  Beside a maximum of 2^10 that rounding, and log2 w's in the sum
+  // with it, are up to 2^-14 each; from there on scores are first taken from the lane's largest, whose product is
+  // rounded as the maximum is, so that no weight passes w however large the scores are.
   __device__ __forceinline__ void softmax(f4 (&sc)[kQ][4], h8 (&pf)[kParts][kQ][2], bool ok, float ks, float vs, int32_t pv) {
     int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
     et = max(et, __shfl_xor(et, 16));
@@ -427,9 +437,19 @@ struct Columns {
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[t][b][r]);
-      const float now = fmaxf(m[t], quarters_max(top * f));
+      const float now = fmaxf(m[t], quarters_max(product(top, f)));
       const float base = now == -INFINITY ? 0.f : now;
-      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, rise), shift = log_w - base;
+      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, rise);
+      float shift = log_w - base;
+      const bool large = fabsf(base) > kLargeScore;
+      if (__any(large)) {  // (what other columns of the wave need changes nothing in this one)
+        const float least = large && top != -INFINITY ? top : 0.f;
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sc[t][b][r] -= least;
+        shift = large ? (product(least, f) - base) + log_w : shift;
+      }
       m[t] = now;
       float sum = 0.f;
 #pragma unroll
