@@ -358,7 +358,7 @@ struct Columns {
   h8 q[kQ][D / 32];
   f4 o[kQ][D / 16];
   float m[kQ], l[kQ];
-  int ev;  // exponent that brings the values' scales seen so far below 1
+  float e[kQ];  // log2 of the largest weight times its values' scale, as of the maximum's
   // Weights go into the second product as one FP16 number each where the result is BF16, whose rounding
   // is eight times coarser, and as two, the number and what its rounding left, where the result is FP16.
   static constexpr int kParts = T == AWE_F16 ? 2 : 1;
@@ -366,7 +366,6 @@ struct Columns {
   __device__ __forceinline__ void begin(const AttendArgs& a, const Seq& s, int head, int64_t first) {
     const int q4 = (threadIdx.x & 63) >> 4, i16 = threadIdx.x & 15;
     col0 = first;
-    ev = -1000;
     cols = (int64_t)s.rows * a.share;
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
@@ -392,7 +391,7 @@ struct Columns {
 #pragma unroll
         for (int e = 0; e < 8; ++e) q[t][j][e] = (_Float16)ldexpf(a.g.scale < 0.f ? -(float)v[j].v[e] : (float)v[j].v[e], 15 - ex);
       factor[t] = ldexpf(fabsf(a.g.scale) * kLog2e, ex - 15);
-      m[t] = -INFINITY;
+      m[t] = e[t] = -INFINITY;
       l[t] = 0.f;
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) o[t][d] = f4{0.f, 0.f, 0.f, 0.f};
@@ -400,21 +399,15 @@ struct Columns {
   }
 
   // Softmax of the lane's 16 tokens (from token pv on) of its column, against the running maximum: scores to
-  // weights.  They lie in one block, so the weights times its values' scale, w = vs 2^(15 - e) < 2^15, are exp2 of
-  // one linear function of the scores, and the weights' sum is theirs over w.  FP16 keeps 11 bits of what is
-  // at least 2^-29 of the largest scale so far, and to 2^-40 of it of the rest.
-  // The running maximum is a rounded product.  Beside a maximum of 2^10 that rounding, and log2 w's in the sum
-  // with it, are up to 2^-14 each; from there on scores are first taken from the lane's largest, whose product is
-  // rounded as the maximum is, so that no weight passes w however large the scores are.
+  // weights.  They lie in one block, so the weights times its values' scale, on the power of two that makes the column's
+  // largest 2^15, are exp2 of one linear function of the scores, and the weights' own sum is theirs by a factor.
+  // FP16 keeps 11 bits of what is at least 2^-29 of the column's largest, and to 2^-40 of it of the rest; what
+  // a column does not see, or gives no weight, takes no part in that.
+  // The running maximum is a rounded product.  Beside a maximum of 2^10 that rounding, and the scales' logarithms'
+  // in the sum with it, are up to 2^-14 each; from there on scores are first taken from the lane's largest, whose
+  // product is rounded as the maximum is, so that no weight passes 2^15 however large the scores are.
   __device__ __forceinline__ void softmax(f4 (&sc)[kQ][4], h8 (&pf)[kParts][kQ][2], bool ok, float ks, float vs, int32_t pv) {
-    int et = vs != 0.f ? __builtin_amdgcn_frexp_expf(vs) : -1000;
-    et = max(et, __shfl_xor(et, 16));
-    et = max(et, __shfl_xor(et, 32));
-    const int e = max(ev, et), rise = ev - e;
-    ev = e;
-    const float w = ldexpf(vs, 15 - e);
-    const bool some = !(w < 0x1p-25f);  // (FP16 holds no smaller weight; but it counts in the sum)
-    const float log_w = some ? __builtin_amdgcn_logf(w) : 0.f, per_w = some ? __builtin_amdgcn_rcpf(w) : 1.f;
+    const float log_vs = (float)__builtin_amdgcn_frexp_expf(vs) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(vs));
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
       float f = factor[t] * ks;
@@ -437,9 +430,15 @@ struct Columns {
       for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[t][b][r]);
-      const float now = fmaxf(m[t], quarters_max(product(top, f)));
+      const float most = product(top, f), now = fmaxf(m[t], quarters_max(most));
       const float base = now == -INFINITY ? 0.f : now;
-      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = ldexpf(drop, rise);
+      const float reach = (most - base) + log_vs;  // log2 of the lane's largest weight times the scale
+      const float held = e[t] + (m[t] - base);
+      e[t] = fmaxf(held, quarters_max(reach));
+      const float ref = e[t] == -INFINITY ? 0.f : e[t];
+      const float drop = __builtin_amdgcn_exp2f(m[t] - base), keep = __builtin_amdgcn_exp2f(held - ref);
+      const bool some = reach > ref - 40.f;  // (FP16 holds no smaller weight; but it counts in the sum)
+      const float log_w = some ? (log_vs - ref) + 15.f : 0.f, per_w = some ? __builtin_amdgcn_exp2f(-log_w) : 1.f;
       float shift = log_w - base;
       const bool large = fabsf(base) > kLargeScore;
       if (__any(large)) {  // (what other columns of the wave need changes nothing in this one)
@@ -481,10 +480,11 @@ struct Columns {
     for (int t = 0; t < kQ; ++t) {
       l[t] += __shfl_xor(l[t], 16);
       l[t] += __shfl_xor(l[t], 32);
+      const float whole = e[t] == -INFINITY ? 0.f : ceilf(e[t]), part = e[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(e[t] - whole);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r], ev - 15);
+        for (int r = 0; r < 4; ++r) o[t][d][r] = ldexpf(o[t][d][r] * part, (int)whole - 15);
     }
   }
 };

@@ -1,4 +1,5 @@
-"""Attention over the int8 cache at the ends of its range, on the GPU against 64 bits: large finite scores."""
+"""Attention over the int8 cache at the ends of its range, on the GPU against 64 bits: large finite scores, and values
+whose blocks differ in size by more than a weight's digits."""
 import numpy as np
 import pytest
 import torch
@@ -17,6 +18,103 @@ def attend(held, table, counts, lengths, q, scale, causal, wide):
         bounds = dict(rows=WIDE, max_rows=WIDE)
         dev = torch.cat([dev, torch.zeros(WIDE - n, *q.shape[1:], dtype=q.dtype, device="cuda")])
     return awe.attend(upload(held), batch_of(counts, lengths, table, **bounds), dev, scale, causal=causal)[:n]
+
+
+def reference(held, blocks, length, q, scale, causal, weight):
+    """One sequence in 64 bits: (out, bound before the result's own rounding), rows x heads x dim.  weight: what the
+    rounding of a weight may be, relative to it.
+
+    R bounds what a token's weight is off by beside that, relative to it: its score's error (as in test_large_scores,
+    with two more roundings for the difference from the maximum), four sums of logarithms of size A at most (the
+    scales' and the 2^15 of FP16), exp2 (an ulp, 2 U) of the weight and of the factor that takes a step's sum to
+    the others', and additions: 32 in a matrix instruction, 64 of waves and parts, and for each step of 64 tokens a
+    rescaling (exp2, two products, the addition: 5 U).  It counts in the numerator and in the denominator.  FP16
+    holds a weighted token to 2^-40 of the row's largest weighted block, times at most 127.  A weight below 2^-126
+    of the largest is no normal number of FP32, and exp2 gives 0 for it: where parts of the tokens meet, such tokens
+    may count as nothing."""
+    n, heads, D = q.shape
+    share = heads // held.heads
+    k, v = held.values(blocks, length, "k"), held.values(blocks, length, "v")
+    of = np.array([int(blocks[p // held.block]) for p in range(length)])
+    out, bound = np.zeros((n, heads, D)), np.zeros((n, heads, D))
+    for i in range(n):
+        see = min(length, length - n + i + 1) if causal else length
+        for h in range(heads if see > 0 else 0):
+            K, V, vs = k[h // share, :see], v[h // share, :see], held.vs[of[:see], h // share].astype(np.float64)
+            score = K @ q[i, h] * scale
+            p = np.exp(score - score.max())
+            p /= p.sum()
+            out[i, h] = p @ V
+            err = (32 + D / 32 + 8) * ref.U * (np.abs(K) @ np.abs(q[i, h]) * abs(scale))
+            A = 15 + 2 * np.abs(np.log2(vs[vs > 0])).max(initial=0)
+            R = err + (4 * A + 4 + 32 + 64 + 5 * see / 64) * ref.U
+            size = (p * (weight + R)) @ np.abs(V) + (p * R).sum() * np.abs(out[i, h])
+            size += np.where(p < 2.0 ** -126 * p.max(), p, 0) @ np.abs(V)
+            bound[i, h] = 1.01 * (size + see * 2.0 ** -40 * (p * vs).max() * 127)
+    return out, bound
+
+
+ONE = 2.0 ** -11  # weights as one FP16 number
+
+
+@pytest.mark.parametrize("new,length,wide", [(1, 200, False), (40, 200, False), (40, 200, True), (1, 5000, False)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("t,ratio", [("bf16", 1e3), ("bf16", 1e9), ("bf16", 1e12), ("bf16", 1e30), ("f16", 1e4)])
+def test_large_values_without_weight_cost_the_others_nothing(t, ratio, dim, new, length, wide):
+    # blocks of large values whose tokens get no weight (scores of -6000 and less), before and among the others
+    block, heads, share = 16, 2, 2
+    nb = -(-length // block) + 1
+    held = ref.Held(nb, heads, dim, block, seed=dim)
+    table = tables([length], block, nb, 2)
+    g = torch.Generator().manual_seed(dim + new)
+    q = (torch.rand(new, heads * share, dim, generator=g) + 0.5).to(T[t])
+    held.k[:] = np.abs(held.k) // 4
+    for b in (0, 5):
+        held.k[table[0][b]] = -127
+        held.ks[table[0][b]] *= 400
+        held.vs[table[0][b]] *= np.float32(ratio)
+    got = attend(held, table, [new], [length], q, 0.5, True, wide)
+    want, bound = reference(held, table[0], length, ref.f64(q), 0.5, True, ONE)
+    assert (np.abs(want) < 10).all() and (bound < 0.02).all()
+    ref.close(got, want, bound, T[t])
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("ratio", [1e3, 1e9, 1e12, 1e30])
+def test_values_of_later_tokens_do_not_reach_earlier_rows(ratio, dim, wide):
+    block, heads, share, length = 16, 1, 2, 200
+    held = ref.Held(14, heads, dim, block, seed=dim)
+    table = tables([length], block, 14, 3)
+    q = torch.randn(length, heads * share, dim, generator=torch.Generator().manual_seed(dim)).bfloat16()
+    clean = attend(held, table, [length], [length], q, 0.125, True, wide)
+    held.vs[table[0][3]] *= np.float32(ratio)  # tokens 48 .. 63
+    held.vs[table[0][8]] *= np.float32(ratio * 1e3)  # tokens 128 .. 143
+    got = attend(held, table, [length], [length], q, 0.125, True, wide)
+    assert torch.equal(got[:48], clean[:48])
+    want, bound = reference(held, table[0], length, ref.f64(q), 0.125, True, ONE)
+    ref.close(got, want, bound, torch.bfloat16)
+
+
+@pytest.mark.parametrize("new,wide", [(1, False), (30, False), (30, True)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_values_from_subnormal_to_large(dim, new, wide):
+    # blocks whose scales span FP32's range, zero among them; each row's weights may fall on any of them
+    block, heads, length = 16, 1, 256
+    held = ref.Held(17, heads, dim, block, seed=dim + 1)
+    table = tables([length], block, 17, 4)
+    for j, power in enumerate((-140, -100, -60, -30, 0, 30, 60, 100, None, -130, 20, -20, 80, -80, 5, -5)):
+        held.vs[table[0][j]] = np.float32(2.0 ** power * 1.3) if power is not None else 0
+    g = torch.Generator().manual_seed(dim + new)
+    q = torch.zeros(new, 16, dim)
+    for h in range(16):  # query head h meets its own block's keys
+        held.k[table[0][h]] = 0
+        held.k[table[0][h], :, :, h] = 100
+        q[:, h, h] = 120 * (0.5 + torch.rand(new, generator=g))
+    q = q.bfloat16()
+    got = attend(held, table, [new], [length], q, 1.0, False, wide)
+    want, bound = reference(held, table[0], length, ref.f64(q), 1.0, False, ONE)
+    ref.close(got, want, bound, torch.bfloat16)
 
 
 @pytest.mark.parametrize("new,length,wide", [(1, 200, False), (1, 9000, False), (20, 200, False), (20, 200, True)])
