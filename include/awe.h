@@ -374,7 +374,7 @@ awe_status awe_cache_load(const awe_cache* cache, const awe_batch* batch, void* 
      out = softmax_j(scale * q . k_j) v_j  over tokens j < lengths[b], and for causal != 0 up to the row's
    own position only.  A row without any token gets zeros.  max_length also sets how the tokens are
    split over workgroups: a bound near the longest length is best.  The weights of the second
-   product are rounded to FP16 (two FP16 numbers each for AWE_F16).  Scores may be as large as FP32
+   product are held as two FP16 numbers each, to 2^-22 of a weight.  Scores may be as large as FP32
    holds (times log2 e); a larger one makes its row NaN, and a row that has only scores below
    that range gets zeros.  The workspace
    (awe_cache_attend_workspace_bytes, aligned to 16 bytes; 0 bytes for most prompts) holds the parts

@@ -281,6 +281,7 @@ __global__ __launch_bounds__(256) void load_kernel(CacheLaunch g) {
 // of two per column that brings the largest below 2^15: what that loses lies 2^-40 below the largest.
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
@@ -359,9 +360,8 @@ struct Columns {
   f4 o[kQ][D / 16];
   float m[kQ], l[kQ];
   float e[kQ];  // log2 of the largest weight times its values' scale, as of the maximum's
-  // Weights go into the second product as one FP16 number each where the result is BF16, whose rounding
-  // is eight times coarser, and as two, the number and what its rounding left, where the result is FP16.
-  static constexpr int kParts = T == AWE_F16 ? 2 : 1;
+  // Weights go into the second product as two FP16 numbers, the weight and what its rounding left, which hold them to 2^-22.
+  static constexpr int kParts = 2;
 
   __device__ __forceinline__ void begin(const AttendArgs& a, const Seq& s, int head, int64_t first) {
     const int q4 = (threadIdx.x & 63) >> 4, i16 = threadIdx.x & 15;
@@ -454,12 +454,18 @@ struct Columns {
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][b][r], f, shift));
-          sum += p;
-          const _Float16 high = (_Float16)p;
-          pf[0][t][b >> 1][4 * (b & 1) + r] = high;
-          if constexpr (kParts == 2) pf[1][t][b >> 1][4 * (b & 1) + r] = (_Float16)(p - (float)high);
+        for (int r = 0; r < 4; r += 2) {
+          const f2 p = {__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][b][r], f, shift)),
+                        __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][b][r + 1], f, shift))};
+          sum += p[0] + p[1];
+          const h2 high = __builtin_convertvector(p, h2);
+          const f2 left = {__builtin_fmaf((float)high[0], -1.f, p[0]), __builtin_fmaf((float)high[1], -1.f, p[1])};
+          const h2 low = __builtin_convertvector(left, h2);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            pf[0][t][b >> 1][4 * (b & 1) + r + i] = high[i];
+            pf[1][t][b >> 1][4 * (b & 1) + r + i] = low[i];
+          }
         }
       l[t] = l[t] * drop + sum * per_w;
       if (__any(!some)) {
@@ -671,9 +677,9 @@ __device__ __forceinline__ void reads_ahead() {
 // Many columns: each of the kW waves has 16 kQ columns, and together they go through the tokens, 64 a step.
 // A step's keys and values become FP16 once per workgroup: a wave fetches its share as it would for itself, and puts the
 // operands into LDS lane by lane, where every wave reads them as they are (twice: a step's while the
-// next one's are on their way).  Bound by vector instructions, softmax's most of all: prompts that
-// take 164 GFLOP run 250-280 us with BF16 results, 340 with FP16 ones, whose weights are two numbers (the FP16 MFMA alone:
-// 131).  Workgroups of 256 columns: 387.
+// next one's are on their way).  Bound by vector instructions, softmax's most of all, and by products: prompts that
+// take 164 GFLOP run 309-316 us (the FP16 MFMA alone: 131, and half as much again for the weights' second numbers;
+// with weights of one number each: 265).  Workgroups of 256 columns were slower (387 instead of 251 before that).
 template <awe_dtype T, int D, int kQ, int kW>
 __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   using Elem = typename RowType<T>::Elem;

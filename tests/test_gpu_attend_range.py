@@ -55,6 +55,7 @@ def reference(held, blocks, length, q, scale, causal, weight):
 
 
 ONE = 2.0 ** -11  # weights as one FP16 number
+TWO = 2.0 ** -22  # as two, the number and what its rounding left
 
 
 @pytest.mark.parametrize("new,length,wide", [(1, 200, False), (40, 200, False), (40, 200, True), (1, 5000, False)])
@@ -149,3 +150,30 @@ def test_large_scores(t, size, scale, dim, new, length, wide):
             room = (2.0 ** -11 + 2 * ref.HALF[T[t]]) * np.abs(near).max()
             assert (got[i, h] >= near.min(0) - room).all() and (got[i, h] <= near.max(0) + room).all(), (i, h)
     assert size * scale < 1e6 or alone > 0  # (the bounds mean something)
+
+
+@pytest.mark.parametrize("new,length,wide", [(1, 200, False), (40, 200, False), (40, 200, True), (1, 5000, False)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+def test_weights_keep_their_digits(t, dim, new, length, wide):
+    # each token's values are the last one's with the other sign, and weights differ little, so that results are far
+    # smaller than the weighted values and their own rounding hides nothing of the weights'
+    block, heads, share = 16, 2, 2
+    nb = -(-length // block) + 1
+    held = ref.Held(nb, heads, dim, block, seed=dim + 2)
+    table = tables([length], block, nb, 5)
+    held.v[..., 1::2] = -held.v[..., ::2]
+    g = torch.Generator().manual_seed(dim + new)
+    q = (torch.randn(new, heads * share, dim, generator=g) * 2).to(T[t])
+    scale = 2.0 ** -7
+    got = attend(held, table, [new], [length], q, scale, False, wide)
+    want, bound = reference(held, table[0], length, ref.f64(q), scale, False, TWO)
+    # weights in one FP16 number would not do, for any column (their roundings average out over 5000 tokens)
+    k, v = held.values(table[0], length, "k"), held.values(table[0], length, "v")
+    for h in range(heads * share if length < 1000 else 0):
+        score = k[h // share] @ ref.f64(q)[0, h] * scale
+        p = np.exp(score - score.max())
+        one = (p * 2 ** 15 * 0.7).astype(np.float16).astype(np.float64) @ v[h // share] / (p.sum() * 2 ** 15 * 0.7)
+        half = ref.HALF[T[t]]
+        assert (np.abs(one - want[0, h]) > bound[0, h] + half * np.abs(want[0, h])).any()
+    ref.close(got, want, bound, T[t])
