@@ -307,7 +307,10 @@ awe_status awe_gemm_crt(int64_t M, int64_t N, int64_t K, const int64_t* A, int64
    points zeros[j*ldz + g] are bytes, and NULL stands for 8 everywhere (codes of -8..7).  x_scales:
    FP32, for AWE_I8 only, NULL for 1.  Y is M x N of y_type (AWE_F32, AWE_BF16, AWE_F16).  Pointers are
    aligned to their element; rows may begin anywhere, less than 16 MiB apart.  K = 0 writes zeros.  A
-   NaN or infinity in a row of X reaches that row of Y alone. */
+   NaN or infinity in a row of X reaches that row of Y alone, as the formula has it.  Where sums in FP32
+   pass its range (infinities among them; group sums of |x| (32 + u + z) past 3.4e38, or scaled ones before the
+   row's scale), the results they touch are computed again in 64 bits, which takes much longer.  A scale
+   that is not finite makes its output not finite. */
 awe_status awe_gemm_w4(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, awe_dtype x_type,
                        const float* x_scales, const uint8_t* W, int64_t ldw, const void* w_scales, int64_t lds,
                        awe_dtype s_type, const uint8_t* zeros, int64_t ldz, int64_t group, void* Y, int64_t ldy,

@@ -161,6 +161,97 @@ __device__ __forceinline__ u4 across_quarters_by_16(u4 w) {
   return u4{c[0], d[0], c[1], d[1]};
 }
 
+// ---- results whose sums in FP32 leave its range ----------------------------------------------
+// With an infinity, or elements so large that 16 and more times them pass FP32's range, sum x (16 + u) and
+// (16 + z) sum x are infinite where the formula's sum need not be.  Such a result is not finite, as no infinity or NaN
+// leaves a sum again, and is computed once more from the formula's terms in 64 bits, which hold them all: a wave
+// takes a result at a time.  A NaN in the row makes NaN either way, so those rows keep what they have.  Bound by the
+// latency of a result's loads: 512 rows against 8192 x 8192 take 0.8 ms with an infinity in one row, 39 ms with one
+// in each and 0.27 ms with a NaN in each (0.09 without either).
+template <awe_dtype T>
+struct Eight {
+  typename Kind<T>::Elem v[8];
+
+  // Elements k .. k + 7 of a row of K, 0 past its end.
+  __device__ __forceinline__ Eight(const typename Kind<T>::Elem* row, uint32_t k, uint32_t K) {
+    if (k + 8 <= K) {
+      *this = __builtin_bit_cast(Eight, load8<T>(row + k));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : 0;
+    }
+  }
+  __device__ __forceinline__ bool has_nan() const {
+    bool nan = false;
+    if constexpr (T != AWE_I8)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) nan |= (v[i] & 0x7fffu) > (T == AWE_BF16 ? 0x7f80u : 0x7c00u);
+    return nan;
+  }
+  __device__ __forceinline__ double value(int i) const {
+    if constexpr (T == AWE_I8) return (double)(int8_t)v[i];
+    if constexpr (T == AWE_BF16) return (double)__builtin_bit_cast(float, (uint32_t)v[i] << 16);
+    return (double)__builtin_bit_cast(_Float16, (uint16_t)v[i]);
+  }
+};
+
+// For the whole wave: whether bad is set and the lane's row m has no NaN.
+template <awe_dtype T>
+__device__ __forceinline__ bool without_nan(const W4Launch& g, bool bad, int64_t m) {
+  if constexpr (T == AWE_I8) return bad;
+  uint64_t left = __ballot(bad), kept = 0;
+  while (left != 0) {
+    const int64_t row = __shfl(m, __builtin_ctzll(left));
+    const uint64_t of_row = __ballot(m == row) & left;
+    left &= ~of_row;
+    const auto* x = reinterpret_cast<const typename Kind<T>::Elem*>(g.x) + row * g.ldx;
+    bool nan = false;
+#pragma unroll 4
+    for (uint32_t k = 8 * (threadIdx.x & 63); k < (uint32_t)g.K; k += 512) nan |= Eight<T>(x, k, (uint32_t)g.K).has_nan();
+    if (!__any(nan)) kept |= of_row;
+  }
+  return kept >> (threadIdx.x & 63) & 1;
+}
+
+// Y[m,j] without its rounding, on every lane.
+template <awe_dtype T>
+__device__ __forceinline__ double by_definition(const W4Launch& g, int64_t m, int64_t j) {
+  const auto* x = reinterpret_cast<const typename Kind<T>::Elem*>(g.x) + m * g.ldx;
+  const uint8_t* w = g.w + j * g.ldw;
+  const uint32_t K = (uint32_t)g.K, group = (uint32_t)g.group;
+  double sum = 0.;
+#pragma unroll 1
+  for (uint32_t k = 8 * (threadIdx.x & 63); k < K; k += 512) {  // (eight indices lie in one group)
+    const int64_t grp = k / group;
+    const float s = g.s_type == AWE_F32    ? reinterpret_cast<const float*>(g.scales)[j * g.lds + grp]
+                    : g.s_type == AWE_BF16 ? (float)reinterpret_cast<const bf16*>(g.scales)[j * g.lds + grp]
+                                           : (float)reinterpret_cast<const f16*>(g.scales)[j * g.lds + grp];
+    const int z = g.zeros != nullptr ? g.zeros[j * g.ldz + grp] : 8;
+    const Eight<T> e(x, k, K);
+    uint8_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = k + 2 * i < K ? w[k / 2 + i] : 0;
+    double part = 0.;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part += e.value(i) * (double)((int)(c[i / 2] >> (4 * (i & 1)) & 15) - z);
+    sum += (double)s * part;
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+  return g.x_scales != nullptr ? sum * (double)g.x_scales[m] : sum;
+}
+
+// For the whole wave: the lanes with bad set get Y[m,j] again.
+template <awe_dtype T>
+__device__ __forceinline__ void store_again(const W4Launch& g, bool bad, int64_t m, int64_t j) {
+#pragma unroll 1
+  for (uint64_t left = __ballot(bad); left != 0; left &= left - 1) {
+    const int lane = __builtin_ctzll(left);
+    const double y = by_definition<T>(g, __shfl(m, lane), __shfl(j, lane));
+    if ((int)(threadIdx.x & 63) == lane) store_real(g.y, m * g.ldy + j, g.y_type, (float)y);
+  }
+}
+
 constexpr int kChunk = 128;  // reduction indices of a wave's step: 16 bytes of codes per lane
 
 struct W4Args {
@@ -425,14 +516,17 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) lds.red[wave][16 * u + 4 * q + r][16 * t + i] = acc[t][u][r];
   __syncthreads();
-  for (int e = threadIdx.x; e < 256 * kM * kN; e += 64 * kW) {
+#pragma unroll 1
+  for (int e = threadIdx.x; e < 256 * kM * kN; e += 64 * kW) {  // (a wave's lanes together)
     const int row = e / (16 * kN), col = e % (16 * kN);
     const int64_t m = m0 + row, j = n0 + col;
-    if (m >= g.M || j >= g.N) continue;
+    const bool ok = m < g.M && j < g.N;
     float v = 0.f;
 #pragma unroll
     for (int k = 0; k < kW; ++k) v += lds.red[k][row][col];
-    store_real(g.y, m * g.ldy + j, g.y_type, g.x_scales != nullptr ? v * g.x_scales[m] : v);
+    if (ok) store_real(g.y, m * g.ldy + j, g.y_type, g.x_scales != nullptr ? v * g.x_scales[m] : v);
+    const bool bad = ok && !__builtin_isfinite(v);
+    if (__any(bad)) store_again<T>(g, without_nan<T>(g, bad, m), m, j);
   }
 }
 
@@ -471,6 +565,7 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
   constexpr int kPieces = kChunk / 8 / kPer;  // pieces of 8 elements each of them has
   static_assert(kPieces == 4, "a thread's pieces make up a step of 32 indices");
   static_assert(kCols <= 256, "a thread per output fetches its scale");
+  static_assert(4 * kM * kN <= 64, "a bit for each of a lane's results");
   const W4Launch& g = a.g;
   const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, q = lane >> 4, i = lane & 15;
@@ -685,6 +780,32 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
       for (int t = 0; t < kN; ++t)
         if (nw + 16 * t + i < g.N) store_real(g.y, m * g.ldy + nw + 16 * t + i, g.y_type, acc[t][u][r] * sx);
     }
+  // (looked through by itself, 4096 rows of 8192 outputs take 713 us; within the stores above, 738)
+  bool odd = false;
+#pragma unroll
+  for (int t = 0; t < kN; ++t)
+#pragma unroll
+    for (int u = 0; u < kM; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) odd |= !__builtin_isfinite(acc[t][u][r]);
+  if (!__any(odd)) return;
+  uint64_t bad = 0;  // bit (4 u + r) kN + t
+#pragma unroll
+  for (int u = 0; u < kM; ++u)
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int t = 0; t < kN; ++t)
+        if (m0 + 16 * u + 4 * q + r < g.M && nw + 16 * t + i < g.N)
+          bad |= (uint64_t)!__builtin_isfinite(acc[t][u][r]) << ((4 * u + r) * kN + t);
+#pragma unroll 1
+  for (int e = 0; e < 4 * kM; ++e) {
+    const uint64_t of_row = ((uint64_t(1) << kN) - 1) << (e * kN);
+    if (!without_nan<T>(g, (bad & of_row) != 0, m0 + 16 * (e / 4) + 4 * q + e % 4)) bad &= ~of_row;
+  }
+#pragma unroll 1
+  for (int e = 0; e < 4 * kM * kN; ++e)
+    store_again<T>(g, bad >> e & 1, m0 + 16 * (e / kN / 4) + 4 * q + e / kN % 4, nw + 16 * (e % kN) + i);
 }
 
 awe_status too_many() {
