@@ -369,7 +369,7 @@ def matmul_crt(A, B, moduli, bound_a, bound_b, d_range_flag=None):
     return c128, c64
 
 
-# ---- quantised inference on torch tensors ------------------------------------------------------
+# ---- quantised inference on torch tensors (for inference: no gradients, tensors that ask for one are refused) ---
 _types = {}  # torch dtype -> awe_dtype
 _REAL, _REAL16, _REAL16_OR_INT8, _INT32 = (F32, BF16, F16), (BF16, F16), (BF16, F16, I8), (I32,)
 _torch = None  # both set when torch is first needed
@@ -394,7 +394,12 @@ def _dtype(t, allowed):
 
 
 def _launch_stream(*tensors):
-    """Handle of the current stream; the library launches on the current device, so the tensors must be there."""
+    """Handle of the current stream; the library launches on the current device, so the tensors must be there, and
+    records nothing for a backward pass, so none may ask for a gradient."""
+    if _torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("no gradient is computed here: detach the tensor, or call under torch.no_grad()")
     if _torch_c is None:
         if any(t is not None and t.get_device() < 0 for t in tensors):
             raise ValueError("a tensor is not on the current device")
@@ -419,7 +424,8 @@ def _rows_2d(t, what):
 def matmul_w4(x, w, scales, group, zeros=None, x_scales=None, out_dtype=None):
     """Y = X W^T for CUDA tensors: x (M x K, bfloat16, float16 or int8), w (N x ceil(K / 2), uint8, two
     codes per byte, the low nibble first), scales and zeros (N x ceil(K / group); zeros uint8 or None
-    for 8), x_scales (M float32, int8 x only).  out_dtype: x's type, bfloat16 for int8, if not given."""
+    for 8), x_scales (M float32, int8 x only).  out_dtype: x's type, bfloat16 for int8, if not given.
+    Computes no gradients."""
     try:
         ((M, K), (ldx, one)), ((N, packed), (ldw, w_one)), (lds, s_one) = \
             (x.shape, x.stride()), (w.shape, w.stride()), scales.stride()
@@ -478,6 +484,8 @@ class Cache:
         for s in (k_scales, v_scales):
             if s.dtype is not _torch.float32 or s.shape != per_head:
                 raise ValueError("scales must be float32 of blocks x heads")
+            if s.requires_grad:
+                raise ValueError("scales are written in place and take no gradient")
         for t in (k, v, k_scales, v_scales):
             if not t.is_contiguous() or t.device != at:
                 raise ValueError("the cache's tensors must be contiguous, and on one device")
@@ -549,7 +557,7 @@ def _flag(t):
 
 
 def store_tokens(cache, batch, k, v, d_range_flag=None):
-    """Stores k and v (rows x heads x dim) as the newest tokens of the batch's sequences."""
+    """Stores k and v (rows x heads x dim) as the newest tokens of the batch's sequences, without gradients."""
     _fits(cache, batch)
     k_row, k_head = _row_tensor(k, cache, batch, cache.heads, "k")
     v_row, v_head = _row_tensor(v, cache, batch, cache.heads, "v")
@@ -576,7 +584,7 @@ def load_tokens(cache, batch, dtype, d_range_flag=None):
 
 def attend(cache, batch, q, scale, causal=True, out=None, d_range_flag=None):
     """Attention of q (rows x query heads x dim) over the cached tokens of the batch's sequences.  Rows that
-    belong to no sequence are not written."""
+    belong to no sequence are not written.  Computes no gradients."""
     _fits(cache, batch)
     heads = q.shape[1] if q.dim() == 3 else 0
     q_row, q_head = _row_tensor(q, cache, batch, heads, "q")
