@@ -133,9 +133,11 @@ awe_status cache_impl(const awe_cache* cache, const awe_batch* batch, const Rows
   return load ? launch_cache_load(g, stream) : launch_cache_store(g, stream);
 }
 
-awe_status check_heads(const awe_cache& c, int32_t q_heads) {
+awe_status check_heads(const awe_cache& c, const awe_batch& b, int32_t q_heads) {
   if (q_heads < 1 || q_heads % c.heads != 0) return invalid("q_heads must be a multiple of the cache's heads");
   if (q_heads > 65535) return refuse(AWE_ERR_UNSUPPORTED, "too many heads");
+  // (so that the plan's counts stay within 64 bits, and its columns within 32)
+  if (std::min(b.rows, b.max_rows) * q_heads > (int64_t(1) << 30)) return refuse(AWE_ERR_UNSUPPORTED, "too many rows");
   return AWE_OK;
 }
 
@@ -144,7 +146,7 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
                        hipStream_t stream) {
   awe_status st = check_cache(cache);
   if (st == AWE_OK) st = check_batch(*cache, batch);
-  if (st == AWE_OK) st = check_heads(*cache, q_heads);
+  if (st == AWE_OK) st = check_heads(*cache, *batch, q_heads);
   if (st != AWE_OK) return st;
   if (type != AWE_BF16 && type != AWE_F16) return invalid("bad type");
   if (empty(*batch)) return AWE_OK;
@@ -153,8 +155,6 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
   if (st == AWE_OK) st = check_rows(o, type);
   if (st != AWE_OK) return st;
   if (!distinct(o, batch->rows, q_heads, cache->head_dim)) return invalid("written elements share memory");
-  if (std::min(batch->rows, batch->max_rows) * q_heads > (int64_t(1) << 30))
-    return refuse(AWE_ERR_UNSUPPORTED, "too many rows");
   const size_t need = plan_attend(*cache, *batch, q_heads).workspace;
   if (need > 0 && (ws == nullptr || ws_bytes < need))
     return refuse(AWE_ERR_WORKSPACE, "workspace smaller than awe_cache_attend_workspace_bytes");
@@ -230,7 +230,7 @@ awe_status awe_cache_attend_workspace_bytes(const awe_cache* cache, const awe_ba
     if (bytes == nullptr) return invalid("bytes is NULL");
     awe_status st = check_cache(cache);
     if (st == AWE_OK) st = check_batch(*cache, batch);
-    if (st == AWE_OK) st = check_heads(*cache, q_heads);
+    if (st == AWE_OK) st = check_heads(*cache, *batch, q_heads);
     if (st == AWE_OK) *bytes = empty(*batch) ? 0 : plan_attend(*cache, *batch, q_heads).workspace;
     return st;
   });
