@@ -412,11 +412,11 @@ struct Columns {
     for (int t = 0; t < kQ; ++t) {
       float f = factor[t] * ks;
       const int32_t see = ok ? last[t] - pv : 0;  // of the lane's tokens, the first so many
-      if (__any(f == 0.f)) {  // (a masked score times 0 would be no number)
+      if (__any(f == 0.f)) {  // (a masked score times 0 would be no number; one of a NaN or an infinity is none)
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) sc[t][b][r] = f == 0.f ? 0.f : sc[t][b][r];
+          for (int r = 0; r < 4; ++r) sc[t][b][r] *= f == 0.f ? 0.f : 1.f;
         f = f == 0.f ? 1.f : f;
       }
       if (__any(see < 16)) {

@@ -177,3 +177,22 @@ def test_weights_keep_their_digits(t, dim, new, length, wide):
         half = ref.HALF[T[t]]
         assert (np.abs(one - want[0, h]) > bound[0, h] + half * np.abs(want[0, h])).any()
     ref.close(got, want, bound, T[t])
+
+
+@pytest.mark.parametrize("new,wide", [(1, False), (40, False), (40, True)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("scale,zero_keys", [(0.0, ()), (0.125, range(7)), (0.125, (6,))])
+def test_non_finite_queries_times_zero_are_no_number(scale, zero_keys, bad, new, wide):
+    # keys of zero (a block's scale is 0) or a scale of 0 do not make a NaN or an infinity of a query disappear
+    held = ref.Held(8, 1, 64, 16, seed=3)
+    table = tables([100], 16, 8, 8)
+    for j in zero_keys:
+        held.ks[table[0][j]] = 0
+    q = torch.randn(new, 2, 64, generator=torch.Generator().manual_seed(1)).bfloat16()
+    clean = attend(held, table, [new], [100], q, scale, True, wide)
+    assert bool(torch.isfinite(clean).all())
+    q[new - 1, 1, 5] = bad  # the newest row: it sees the last block, too
+    got = attend(held, table, [new], [100], q, scale, True, wide)
+    assert bool(torch.isnan(got[new - 1, 1]).all())
+    got[new - 1, 1] = clean[new - 1, 1]
+    assert torch.equal(got, clean)
