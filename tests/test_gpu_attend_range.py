@@ -196,3 +196,24 @@ def test_non_finite_queries_times_zero_are_no_number(scale, zero_keys, bad, new,
     assert bool(torch.isnan(got[new - 1, 1]).all())
     got[new - 1, 1] = clean[new - 1, 1]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dim,t", [(64, "bf16"), (128, "f16"), (256, "bf16")])
+def test_rows_do_not_depend_on_the_calls_others(dim, t):
+    # the rows kernel: a column's sums do not depend on its tile, nor on what its neighbours are
+    held = ref.Held(30, 2, dim, 16, seed=dim)
+    lengths, counts = [300, 150], [40, 33]
+    table = tables(lengths, 16, 30, 9)
+    q = torch.randn(73, 6, dim, generator=torch.Generator().manual_seed(2)).to(T[t])
+    got = attend(held, table, counts, lengths, q, 0.1, True, True)
+    for first, count, seq, length in ((0, 40, 0, 300), (40, 33, 1, 150), (39, 1, 0, 300), (60, 13, 1, 150)):
+        alone = attend(held, table[seq: seq + 1], [count], [length], q[first: first + count], 0.1, True, True)
+        assert torch.equal(alone, got[first: first + count]), first
+    # one row as a sequence of its own, and neighbours that are large, infinite and NaN
+    pair = attend(held, table[[0, 0]], [1, 1], [300, 300], q[[39, 39]], 0.1, True, True)
+    assert torch.equal(pair[0], got[39]) and torch.equal(pair[1], got[39])
+    odd = q.clone()
+    odd[::3] = (odd[::3].float() * 30000).to(T[t])
+    odd[1::3, ::2], odd[1::3, 1::2] = float("inf"), float("nan")
+    keep = list(range(2, 73, 3))
+    assert torch.equal(attend(held, table, counts, lengths, odd, 0.1, True, True)[keep], got[keep])
