@@ -376,10 +376,13 @@ awe_status awe_cache_load(const awe_cache* cache, const awe_batch* batch, void* 
    type AWE_BF16 or AWE_F16, strides as above:
      out = softmax_j(scale * q . k_j) v_j  over tokens j < lengths[b], and for causal != 0 up to the row's
    own position only.  A row without any token gets zeros.  max_length also sets how the tokens are
-   split over workgroups: a bound near the longest length is best.  The weights of the second
-   product are held as two FP16 numbers each, to 2^-22 of a weight.  Scores may be as large as FP32
-   holds (times log2 e); a larger one makes its row NaN, and a row that has only scores below
-   that range gets zeros.  The workspace
+   split over workgroups: a bound near the longest length is best.  max_rows decides for the whole call
+   whether tokens are split at all: prompts, and sequences of few rows over many tokens, are best
+   two calls (2048 rows beside one row over 65,536 tokens: 2.8 ms together, 0.15 apart).  The weights of
+   the second product are held as two FP16 numbers each, to 2^-22 of a weight and 2^-40 of a row's largest
+   weight times its values' scale.  Scores (times log2 e) and a row's sum of weights, relative to its
+   largest, times values stay within FP32's range; a larger score makes its row NaN, and a row that has
+   only scores below that range gets zeros.  The workspace
    (awe_cache_attend_workspace_bytes, aligned to 16 bytes; 0 bytes for most prompts) holds the parts
    of split sequences until the call's kernels have run. */
 awe_status awe_cache_attend_workspace_bytes(const awe_cache* cache, const awe_batch* batch, int32_t q_heads,

@@ -584,7 +584,8 @@ def load_tokens(cache, batch, dtype, d_range_flag=None):
 
 def attend(cache, batch, q, scale, causal=True, out=None, d_range_flag=None):
     """Attention of q (rows x query heads x dim) over the cached tokens of the batch's sequences.  Rows that
-    belong to no sequence are not written.  Computes no gradients."""
+    belong to no sequence are not written.  out shares no memory with q.  Prompts, and sequences of few rows
+    over many tokens, are best two calls.  Computes no gradients."""
     _fits(cache, batch)
     heads = q.shape[1] if q.dim() == 3 else 0
     q_row, q_head = _row_tensor(q, cache, batch, heads, "q")

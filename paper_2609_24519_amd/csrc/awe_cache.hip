@@ -11,8 +11,8 @@ namespace {
 // leads to them (starts and lengths, table, rows, then the largest); for 4544 rows of 8 heads of 128 in
 // BF16, storing takes 12 us (28 MB, 2.3 TB/s), loading 8 (28 MB, 3.5 TB/s).  A thread has up to kPatches
 // patches of four adjacent tokens by eight dimensions; storing keeps them in registers between the search for
-// the largest and the rounding, so rows are read once (reading them twice, and dividing by the scale: 18.6 us).  Values, which are kept by dimension, are turned over in
-// LDS, a word of four tokens at a time.
+// the largest and the rounding, so rows are read once (reading them twice, and dividing by the scale: 18.6 us).
+// Values, which are kept by dimension, are turned over in LDS, a word of four tokens at a time.
 struct Tile {
   int32_t id, t0, t1;  // block (-1: nothing to do), slots that get rows
   int64_t row0;        // row of slot 0 (of slot t0 at the earliest)
@@ -360,7 +360,8 @@ struct Columns {
   f4 o[kQ][D / 16];
   float m[kQ], l[kQ];
   float e[kQ];  // log2 of the largest weight times its values' scale, as of the maximum's
-  // Weights go into the second product as two FP16 numbers, the weight and what its rounding left, which hold them to 2^-22.
+  // Weights go into the second product as two FP16 numbers, the weight and what its rounding left, which hold
+  // them to 2^-22 of a weight (and to 2^-40 of the column's largest).
   static constexpr int kParts = 2;
 
   __device__ __forceinline__ void begin(const AttendArgs& a, const Seq& s, int head, int64_t first) {
@@ -538,8 +539,9 @@ struct Tokens {
 
 // Few columns: a workgroup has 16 of them and a chunk of the tokens, which its waves take 64 at a time in
 // turn.  Bound by the cache's bytes: a wave has a step's keys and values in flight while it works on
-// the step before.  64 sequences of up to 8192 tokens, 8 heads of 128: 117 us (549 MB, 4.7 TB/s; a copy reaches 5.2);
-// one sequence of 65,536: 27 us (134 MB, 4.9 TB/s).
+// the step before.  Traced, 64 sequences of up to 8192 tokens, 8 heads of 128, take 119 us (549 MB, 4.6 TB/s; a copy
+// reaches 5.2), one sequence of 65,536 28 us (134 MB, 4.8 TB/s).  It goes through all tokens, also those
+// that a causal row does not see: rows are few here.
 template <awe_dtype T, int D>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void attend_split_kernel(AttendArgs a) {
   using Elem = typename RowType<T>::Elem;
@@ -677,9 +679,10 @@ __device__ __forceinline__ void reads_ahead() {
 // Many columns: each of the kW waves has 16 kQ columns, and together they go through the tokens, 64 a step.
 // A step's keys and values become FP16 once per workgroup: a wave fetches its share as it would for itself, and puts the
 // operands into LDS lane by lane, where every wave reads them as they are (twice: a step's while the
-// next one's are on their way).  Bound by vector instructions, softmax's most of all, and by products: prompts that
-// take 164 GFLOP run 309-316 us (the FP16 MFMA alone: 131, and half as much again for the weights' second numbers;
-// with weights of one number each: 265).  Workgroups of 256 columns were slower (387 instead of 251 before that).
+// next one's are on their way).  Bound by vector instructions, softmax's most of all (61 % of a CU's busy cycles), and
+// by products (36 %): calls back to back, prompts that take 164 GFLOP run 308-316 us (the FP16 MFMA alone: 131, and
+// half as much again for the weights' second numbers; with weights of one number each: 265).  Workgroups of 256
+// columns were slower (387 instead of 251, with one number).
 template <awe_dtype T, int D, int kQ, int kW>
 __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(AttendArgs a) {
   using Elem = typename RowType<T>::Elem;
@@ -689,7 +692,7 @@ __global__ __launch_bounds__(64 * kW, D == 256 ? 1 : 2) void attend_rows_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q4 = lane >> 4, i16 = lane & 15;
   // The last columns see the most tokens: they go first.  Heads are next to each other, so that with
   // eight of them the workgroups of a head, which read the same tokens, are on one XCD (293 us instead of
-  // 316 for prompts of up to 2048 tokens; all sequences' last columns first took 491).
+  // 316 for prompts of up to 2048 tokens, as the kernel was then; all sequences' last columns first took 491).
   const uint32_t per_seq = (uint32_t)a.col_groups * a.g.c.heads, in = blockIdx.x % per_seq;
   const int head = in % a.g.c.heads, sid = blockIdx.x / per_seq, group = a.col_groups - 1 - (int)(in / a.g.c.heads);
   const Seq s = sequence(a.g.b, sid, false, a.g.flag, threadIdx.x == 0 && group == 0);

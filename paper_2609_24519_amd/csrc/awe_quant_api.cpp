@@ -165,11 +165,19 @@ awe_status attend_impl(const awe_cache* cache, const awe_batch* batch, const Row
 
 }  // namespace
 
-// Per 64 tokens, a workgroup whose four waves have columns of their own (128 of them) takes 2.0 us while each has a CU
-// to itself and 3.4 us with two on a CU; 16 columns whose tokens are split over waves take 2.2 us of one of 2048 waves.
-// So splitting wins while there are few tiles of 16 columns (measured, 8 heads of 128: 8 sequences of 2048 tokens,
-// 64 columns each 32 us instead of 80, 256 columns 89 instead of 77; one of 8192, 1024 columns 143 instead of 256;
-// 64 of 2048, 64 columns 190 instead of 115), or where columns leave most of a tile of 128 empty.
+// Columns of their own read each token once for 128 columns, but a workgroup goes through all of a sequence; 16 columns
+// whose tokens are split over waves and workgroups read it eight times as often.  So splitting wins while there are
+// few tiles of 16 columns, or where columns leave most of a tile of 128 empty.  In us, split / own columns, 8 heads
+// of 64, 128 and 256:
+//   8 sequences of 2048, 64 columns each     22 /  80    33 /  96    59 / 115
+//   8 of 2048, 256 (1024 tiles)              52 /  75    79 /  93   175 / 125
+//   1 of 8192, 1024 (512 tiles)              82 / 264   140 / 322   327 / 416
+//   1 of 8192, 2048 (1024 tiles)            138 / 264   231 / 321   523 / 418
+//  64 of 2048, 8                             33 / 100    52 / 128   124 / 251
+//  64 of 2048, 64 (2048 tiles)               97 / 100   178 / 132   406 / 256
+// (Heads of 64 and 128 would gain from splitting a little beyond the 900 tiles, heads of 256 lose from there on.)
+// The choice is the batch's, by max_rows: a prompt beside sequences of few rows makes all of them go the prompt's way
+// (2048 rows and one row over 65,536 tokens, 8 heads of 128: 2805 us in one call, 110 and 35 in two).
 AttendPlan plan_attend(const awe_cache& c, const awe_batch& b, int32_t q_heads) {
   constexpr int64_t kFewTiles = 900, kTilesPerWide = 3;
   constexpr int64_t kFill = 4096;   // workgroups that keep the chip busy to the end of ragged sequences

@@ -320,7 +320,8 @@ __device__ __forceinline__ float scale_value(uint32_t raw) {
 
 // Bytes of a row as they are loaded.  kOdd: at any address, as the words that hold them (the last one may be one
 // more), put together when they are used; the memory system takes about twice as long for wide loads at addresses
-// that are not multiples of 4.
+// that are not multiples of 4.  Up to three bytes on either side of the operand are read with its first and last
+// word and not used: an aligned word that holds a byte of the operand lies in that byte's page.
 template <int kBytes, bool kOdd>
 struct Piece {
   static constexpr int kN = kBytes / 4;
@@ -346,9 +347,9 @@ __device__ __forceinline__ uint32_t in_word(const uint8_t* p) { return (uint32_t
 // Few rows, or few outputs: 16 kN outputs per workgroup, whose kW waves take the chunks of the reduction in turn, each
 // with up to kM x 16 rows of X.  Operands go straight from memory to the matrix unit, and a wave's loop is one
 // copy of the code for kD chunks, whose loads the compiler spreads over the products.  Bound by the weights' bytes
-// and the loads' latency: one row at 8192 x 8192 takes 11.2 us (35 MB, 3.1 TB/s), 16 int8 rows 12.6.  Unrolled
-// further to fetch ahead, it spends more time on fetching instructions than it saves (13.2 us for one
-// row; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
+// and the loads' latency: calls back to back, one row at 8192 x 8192 takes 11.2 us (35 MB, 3.1 TB/s; traced by
+// itself 11.9), 16 int8 rows 12.7 (12.6).  Unrolled further to fetch ahead, it spends more time on fetching
+// instructions than it saves (13.2 us for one row; X staged in LDS: 13.2; 16 outputs per workgroup: 14.3).
 constexpr int kW = 8;
 
 // S: the scales' type, or kAnyScale for the one that the call says (one row at 8192 x 8192: 14.1 us instead of 11.2).
@@ -532,13 +533,15 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
 
 // Many rows: a workgroup has 16 kM rows and 64 kN outputs, 16 kN of them each of its four waves, and goes
 // through the reduction chunk by chunk.  The rows of X lie in LDS, twice (one chunk is multiplied while the
-// next one is put there in the order of the codes, and the one after that is on its way), together with what the codes' bias makes of each
-// row, -(bias + 8) sum x over a group, which is where a group's sum starts; scales and zero points lie there
-// too, as floats.  A wave's weights go from memory to its registers, and no other wave unpacks them.
+// next one is put there in the order of the codes, and the one after that is on its way), together with what
+// the codes' bias makes of each row, -(bias + 8) sum x over a group, which is where a group's sum starts; scales
+// and zero points lie there too, as floats.  A wave's weights go from memory to its registers, and no other
+// wave unpacks them.
 // kG groups of four waves take the chunks in turn, each with X of its own in LDS, and add up at the end, so that
-// a CU with one workgroup has two waves per SIMD, too.  Bound by vector instructions (half the cycles, for
-// the codes and the folding; MFMAs take a third), at the two waves per SIMD that the registers allow: BF16 rows
-// against 8192 x 8192 take 93 us for 512 (740 TFLOP/s) and 715-760 for 4096 (720-770; a plain product of BF16 numbers reaches 1250).
+// a CU with one workgroup has two waves per SIMD, too.  Bound by vector instructions (58 % of a CU's busy cycles for
+// 4096 rows with zero points, for the codes and the folding; MFMAs are busy for 34 %), at the two waves per SIMD that
+// the registers allow: calls back to back, BF16 rows against 8192 x 8192 take 93 us for 512 (740 TFLOP/s; traced
+// by itself 106) and 711-722 for 4096 (760-770; a plain product of BF16 numbers reaches 1250).
 template <awe_dtype T, int kM, int kN, int kFold>
 struct TileLds {  // of a group of waves
   using X = Kind<T>;
@@ -867,8 +870,13 @@ awe_status launch_tiles(const W4Args& a, hipStream_t stream) {
 template <awe_dtype T, int kFold>
 awe_status launch_kind(const W4Args& a, hipStream_t stream) {
   // Up to 64 rows, and more while workgroups of 32 x 32 are at most two for each of the 256 CUs: these split the
-  // reduction over eight waves, a tile over two groups (BF16, K = 8192: 128 x 128 19 us instead of 43, 512 x 1024
-  // 43 instead of 52, but 1024 x 1024 80 instead of 53; K = 512: 4.5 / 8.8, 7.8 / 9.0, 13.4 / 9.3).
+  // reduction over eight waves, a tile over two groups.  In us, split / tile, of BF16 rows, int8 ones, BF16 with
+  // groups of 32, and BF16 against rows of W off words:
+  //   128 x  128 x 8192   19 / 43   12 / 35   20 / 73   20 / 55
+  //   512 x 1024 x 8192   43 / 53   30 / 41   50 / 97   48 / 65
+  //  1024 x 1024 x 8192   80 / 53   54 / 41   97 / 98   94 / 65
+  //  1024 x 1024 x  512   13 / 10   10 /  9   19 / 12   17 / 10
+  //    64 x 8192 x 8192   44 / 49   30 / 38   50 / 94   49 / 66
   if (a.g.M > 64 && ((a.g.N + 31) / 32) * ((a.g.M + 31) / 32) > 512) return launch_tiles<T, kFold>(a, stream);
   // 16 outputs a workgroup while that is at most one per CU (M = 1: 8.4 us instead of 10.4 at 4096 x 8192,
   // but 12.3 instead of 10.9 at 8192 x 8192); beyond, 32 halve what is read of X
