@@ -309,7 +309,7 @@ awe_status awe_gemm_crt(int64_t M, int64_t N, int64_t K, const int64_t* A, int64
    aligned to their element; rows may begin anywhere, less than 16 MiB apart.  K = 0 writes zeros.  A
    NaN or infinity in a row of X reaches that row of Y alone, as the formula has it.  Where sums in FP32
    pass its range (infinities among them; group sums of |x| (32 + u + z) past 3.4e38, or scaled ones before the
-   row's scale), the results they touch are computed again in 64 bits, which takes much longer.  A scale
+   row's scale), the results they touch are computed again, which takes longer.  A scale
    that is not finite makes its output not finite. */
 awe_status awe_gemm_w4(int64_t M, int64_t N, int64_t K, const void* X, int64_t ldx, awe_dtype x_type,
                        const float* x_scales, const uint8_t* W, int64_t ldw, const void* w_scales, int64_t lds,

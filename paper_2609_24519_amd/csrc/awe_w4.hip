@@ -164,10 +164,10 @@ __device__ __forceinline__ u4 across_quarters_by_16(u4 w) {
 // ---- results whose sums in FP32 leave its range ----------------------------------------------
 // With an infinity, or elements so large that 16 and more times them pass FP32's range, sum x (16 + u) and
 // (16 + z) sum x are infinite where the formula's sum need not be.  Such a result is not finite, as no infinity or NaN
-// leaves a sum again, and is computed once more from the formula's terms in 64 bits, which hold them all: a wave
-// takes a result at a time.  A NaN in the row makes NaN either way, so those rows keep what they have.  Bound by the
-// latency of a result's loads: 512 rows against 8192 x 8192 take 0.8 ms with an infinity in one row, 39 ms with one
-// in each and 0.27 ms with a NaN in each (0.09 without either).
+// leaves a sum again, and is computed once more: in a row with a NaN it is NaN either way, in a row with infinities
+// their terms decide, and otherwise a wave adds the formula's terms in 64 bits, which hold them all, a result at a time.
+// Bound by the latency of loads: 512 rows against 8192 x 8192 (0.09 ms) take 0.14 ms with an infinity in one row, 1.9
+// with one in each, 0.34 with a NaN in each, 0.8 with one row of elements near 2^122 and 40 with all of them such.
 template <awe_dtype T>
 struct Eight {
   typename Kind<T>::Elem v[8];
@@ -181,12 +181,14 @@ struct Eight {
       for (int i = 0; i < 8; ++i) v[i] = k + i < K ? row[k + i] : 0;
     }
   }
-  __device__ __forceinline__ bool has_nan() const {
-    bool nan = false;
+  // Of its elements: bit i if the i-th is an infinity, bit 8 if one is a NaN.
+  __device__ __forceinline__ uint32_t special() const {
+    constexpr uint32_t infinity = T == AWE_BF16 ? 0x7f80u : 0x7c00u;
+    uint32_t r = 0;
     if constexpr (T != AWE_I8)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) nan |= (v[i] & 0x7fffu) > (T == AWE_BF16 ? 0x7f80u : 0x7c00u);
-    return nan;
+      for (int i = 0; i < 8; ++i) r |= (v[i] & 0x7fffu) == infinity ? 1u << i : (v[i] & 0x7fffu) > infinity ? 256u : 0u;
+    return r;
   }
   __device__ __forceinline__ double value(int i) const {
     if constexpr (T == AWE_I8) return (double)(int8_t)v[i];
@@ -195,22 +197,14 @@ struct Eight {
   }
 };
 
-// For the whole wave: whether bad is set and the lane's row m has no NaN.
-template <awe_dtype T>
-__device__ __forceinline__ bool without_nan(const W4Launch& g, bool bad, int64_t m) {
-  if constexpr (T == AWE_I8) return bad;
-  uint64_t left = __ballot(bad), kept = 0;
-  while (left != 0) {
-    const int64_t row = __shfl(m, __builtin_ctzll(left));
-    const uint64_t of_row = __ballot(m == row) & left;
-    left &= ~of_row;
-    const auto* x = reinterpret_cast<const typename Kind<T>::Elem*>(g.x) + row * g.ldx;
-    bool nan = false;
-#pragma unroll 4
-    for (uint32_t k = 8 * (threadIdx.x & 63); k < (uint32_t)g.K; k += 512) nan |= Eight<T>(x, k, (uint32_t)g.K).has_nan();
-    if (!__any(nan)) kept |= of_row;
-  }
-  return kept >> (threadIdx.x & 63) & 1;
+// A scale and a zero point as the formula has them.
+__device__ __forceinline__ float scale_at(const W4Launch& g, int64_t j, int64_t grp) {
+  return g.s_type == AWE_F32    ? reinterpret_cast<const float*>(g.scales)[j * g.lds + grp]
+         : g.s_type == AWE_BF16 ? (float)reinterpret_cast<const bf16*>(g.scales)[j * g.lds + grp]
+                                : (float)reinterpret_cast<const f16*>(g.scales)[j * g.lds + grp];
+}
+__device__ __forceinline__ int zero_at(const W4Launch& g, int64_t j, int64_t grp) {
+  return g.zeros != nullptr ? g.zeros[j * g.ldz + grp] : 8;
 }
 
 // Y[m,j] without its rounding, on every lane.
@@ -223,10 +217,8 @@ __device__ __forceinline__ double by_definition(const W4Launch& g, int64_t m, in
 #pragma unroll 1
   for (uint32_t k = 8 * (threadIdx.x & 63); k < K; k += 512) {  // (eight indices lie in one group)
     const int64_t grp = k / group;
-    const float s = g.s_type == AWE_F32    ? reinterpret_cast<const float*>(g.scales)[j * g.lds + grp]
-                    : g.s_type == AWE_BF16 ? (float)reinterpret_cast<const bf16*>(g.scales)[j * g.lds + grp]
-                                           : (float)reinterpret_cast<const f16*>(g.scales)[j * g.lds + grp];
-    const int z = g.zeros != nullptr ? g.zeros[j * g.ldz + grp] : 8;
+    const float s = scale_at(g, j, grp);
+    const int z = zero_at(g, j, grp);
     const Eight<T> e(x, k, K);
     uint8_t c[4];
 #pragma unroll
@@ -241,11 +233,72 @@ __device__ __forceinline__ double by_definition(const W4Launch& g, int64_t m, in
   return g.x_scales != nullptr ? sum * (double)g.x_scales[m] : sum;
 }
 
-// For the whole wave: the lanes with bad set get Y[m,j] again.
+// Y[m,j] of the lanes with mine set, each with its j, for a row m with infinities: their terms alone, as the
+// others' sum is finite.
 template <awe_dtype T>
-__device__ __forceinline__ void store_again(const W4Launch& g, bool bad, int64_t m, int64_t j) {
+__device__ __forceinline__ float by_infinities(const W4Launch& g, bool mine, int64_t m, int64_t j) {
+  const auto* x = reinterpret_cast<const typename Kind<T>::Elem*>(g.x) + m * g.ldx;
+  const uint32_t K = (uint32_t)g.K, mine_at = 8 * (threadIdx.x & 63);
+  float sum = 0.f;
 #pragma unroll 1
-  for (uint64_t left = __ballot(bad); left != 0; left &= left - 1) {
+  for (uint32_t k0 = 0; k0 < K; k0 += 512) {
+    const uint32_t special = k0 + mine_at < K ? Eight<T>(x, k0 + mine_at, K).special() : 0;
+#pragma unroll 1
+    for (uint64_t lanes = __ballot(special != 0); lanes != 0; lanes &= lanes - 1) {
+      const int from = __builtin_ctzll(lanes);
+#pragma unroll 1
+      for (uint32_t bits = __shfl(special, from); bits != 0; bits &= bits - 1) {
+        const uint32_t k = k0 + 8 * from + __builtin_ctz(bits);
+        if (mine) {
+          const int64_t grp = k / (uint32_t)g.group;
+          const int code = g.w[j * g.ldw + k / 2] >> (4 * (k & 1)) & 15;
+          const float infinity = x[k] >> 15 ? -INFINITY : INFINITY;
+          sum += scale_at(g, j, grp) * (infinity * (float)(code - zero_at(g, j, grp)));
+        }
+      }
+      if (!__any(mine && sum == sum)) return sum;  // NaN in all of them, and it stays
+    }
+  }
+  return sum;
+}
+
+// For the whole wave: what a lane's Y[m,j] with bad set takes.
+enum class Again { kNothing, kDefinition, kInfinities };
+template <awe_dtype T>
+__device__ __forceinline__ Again again(const W4Launch& g, bool bad, int64_t m) {
+  if constexpr (T == AWE_I8) return bad ? Again::kDefinition : Again::kNothing;
+  uint64_t left = __ballot(bad), finite = 0, infinite = 0;
+  while (left != 0) {
+    const int64_t row = __shfl(m, __builtin_ctzll(left));
+    const uint64_t of_row = __ballot(m == row) & left;
+    left &= ~of_row;
+    const auto* x = reinterpret_cast<const typename Kind<T>::Elem*>(g.x) + row * g.ldx;
+    uint32_t special = 0;
+#pragma unroll 4
+    for (uint32_t k = 8 * (threadIdx.x & 63); k < (uint32_t)g.K; k += 512) special |= Eight<T>(x, k, (uint32_t)g.K).special();
+    if (__any(special >= 256)) continue;  // a NaN
+    (__any(special != 0) ? infinite : finite) |= of_row;
+  }
+  const uint64_t me = uint64_t(1) << (threadIdx.x & 63);
+  return infinite & me ? Again::kInfinities : finite & me ? Again::kDefinition : Again::kNothing;
+}
+
+// For the whole wave: Y[m,j] again.
+template <awe_dtype T>
+__device__ __forceinline__ void store_again(const W4Launch& g, Again how, int64_t m, int64_t j) {
+  if constexpr (T != AWE_I8) {
+    uint64_t left = __ballot(how == Again::kInfinities);
+#pragma unroll 1
+    while (left != 0) {
+      const int64_t row = __shfl(m, __builtin_ctzll(left));
+      const bool mine = how == Again::kInfinities && m == row;
+      left &= ~__ballot(mine);
+      const float y = by_infinities<T>(g, mine, row, j);
+      if (mine) store_real(g.y, m * g.ldy + j, g.y_type, y);
+    }
+  }
+#pragma unroll 1
+  for (uint64_t left = __ballot(how == Again::kDefinition); left != 0; left &= left - 1) {
     const int lane = __builtin_ctzll(left);
     const double y = by_definition<T>(g, __shfl(m, lane), __shfl(j, lane));
     if ((int)(threadIdx.x & 63) == lane) store_real(g.y, m * g.ldy + j, g.y_type, (float)y);
@@ -527,7 +580,7 @@ __global__ __launch_bounds__(64 * kW, 2) void w4_rows_kernel(W4Args a) {
     for (int k = 0; k < kW; ++k) v += lds.red[k][row][col];
     if (ok) store_real(g.y, m * g.ldy + j, g.y_type, g.x_scales != nullptr ? v * g.x_scales[m] : v);
     const bool bad = ok && !__builtin_isfinite(v);
-    if (__any(bad)) store_again<T>(g, without_nan<T>(g, bad, m), m, j);
+    if (__any(bad)) store_again<T>(g, again<T>(g, bad, m), m, j);
   }
 }
 
@@ -803,12 +856,13 @@ __global__ __launch_bounds__(256 * kG, 2) void w4_tile_kernel(W4Args a) {
           bad |= (uint64_t)!__builtin_isfinite(acc[t][u][r]) << ((4 * u + r) * kN + t);
 #pragma unroll 1
   for (int e = 0; e < 4 * kM; ++e) {
-    const uint64_t of_row = ((uint64_t(1) << kN) - 1) << (e * kN);
-    if (!without_nan<T>(g, (bad & of_row) != 0, m0 + 16 * (e / 4) + 4 * q + e % 4)) bad &= ~of_row;
-  }
+    const uint32_t of_row = (uint32_t)(bad >> (e * kN)) & ((1u << kN) - 1);
+    if (!__any(of_row != 0)) continue;
+    const int64_t m = m0 + 16 * (e / 4) + 4 * q + e % 4;
+    const Again how = again<T>(g, of_row != 0, m);
 #pragma unroll 1
-  for (int e = 0; e < 4 * kM * kN; ++e)
-    store_again<T>(g, bad >> e & 1, m0 + 16 * (e / kN / 4) + 4 * q + e / kN % 4, nw + 16 * (e % kN) + i);
+    for (int t = 0; t < kN; ++t) store_again<T>(g, of_row >> t & 1 ? how : Again::kNothing, m, nw + 16 * t + i);
+  }
 }
 
 awe_status too_many() {

@@ -128,3 +128,20 @@ def test_infinities_under_capture_and_in_strided_rows(M, N):
         check(d, K, group, "f32", [M // 2, M - 1])
         eager = awe.matmul_w4(d["x"], d["w"], d["scales"], group, d["zeros"], None, torch.float32)
         assert torch.equal(torch.nan_to_num(y, nan=1.25), torch.nan_to_num(eager, nan=1.25))
+
+
+@pytest.mark.parametrize("M,N", SIZES)
+@pytest.mark.parametrize("x,K,group", [("bf16", 1100, 128), ("f16", 515, 64), ("bf16", 650, 32)])
+def test_rows_of_infinities(M, N, x, K, group):
+    # whole rows of infinities: their sign where all codes lie on one side of the zero point, times the scale's
+    d = inputs(M, N, K, group, x, "f32", False, seed=M + K + 2)
+    d["w"][0::5], d["w"][1::5], d["w"][2::5] = 0xff, 0x00, 0x88
+    d["scales"][0::10] *= -1
+    d["scales"][4::20, 0] = 0
+    special = sorted({0, M - 1, M // 2})
+    for i, r in enumerate(special):
+        d["x"][r] = float("-inf") if i % 2 else float("inf")
+        if i == 2:
+            d["x"][r, : K // 2] = 1.0  # infinities in the second half alone
+    want = check(d, K, group, "f32", special)
+    assert np.isposinf(want).any() and np.isneginf(want).any() and np.isnan(want).any()
